@@ -13,7 +13,9 @@
  * Around them: vegas_select_tokens (the paper's own granularity: single tokens from averaged logits, Sec. 3.3);
  * vegas_append_kv, vegas_extend_selection and vegas_append_kv_extend (the step between two draft calls of a live
  * drafting phase: Sec. 2.3, Sec. 3.2 last sentence) and vegas_draft_step (that step with its draft call);
- * vegas_draft_attention_static (the draft call for callers that cannot allocate device memory); vegas_init,
+ * vegas_draft_attention_static (the draft call for callers that cannot allocate device memory); the path over an 8-bit cache
+ * (vegas_append_quant, vegas_read_quant, vegas_verify_attention_quant, vegas_draft_attention_quant) and rotary positions
+ * (vegas_rope_frequencies, vegas_rotate); vegas_init,
  * vegas_workspace_bytes, vegas_strerror; and the vegas_debug_* entry points (parts of a call for benchmarks, a table
  * checker, a plain-read yardstick, phase stamps of profiling builds).
  *
@@ -31,7 +33,7 @@
  *     into [0, num_pages) and lengths into [0, max_seq_len] on the device, so a corrupt table or
  *     length cannot fault; results are then unspecified.
  *   - `workspace` is caller-owned device scratch of at least vegas_workspace_bytes(desc) bytes,
- *     256-byte aligned.  Its contents are meaningless between calls; calls that share a workspace
+ *     256-byte aligned (calls over an 8-bit cache: vegas_quant_workspace_bytes).  Its contents are meaningless between calls; calls that share a workspace
  *     must be ordered on one stream.
  *   - vegas_init() is optional but recommended once per device before the first call: it does the
  *     one-time, per-device set-up (compute-unit count, raised LDS limits of the large kernels) that
@@ -316,6 +318,132 @@ int vegas_draft_attention_static(const vegas_desc* desc, const void* q, const vo
 
 /* Size in bytes of the built-in scratch array that vegas_draft_attention_static uses. */
 size_t vegas_static_scratch_bytes(void);
+
+/* ---------------------------------------------------------------------------------------------------------------------
+ * An 8-bit K/V cache, and rotary positions.
+ *
+ * The cache has the layout of the bf16 caches (NHD pages with the descriptor's strides), with elements of one byte: strides
+ * are then bytes, and multiples of 16 here.  A row -- one token's K or V of one KV head, x[0 .. D) with a = max |x| -- is stored
+ * as D codes round(x * (top * (1 / a))), to nearest even, and one fp32 scale a * (1 / top) (every product and reciprocal rounded
+ * to fp32): value = code * scale.
+ *   VEGAS_QUANT_E4M3   codes are e4m3 (4 exponent, 3 mantissa bits, finite up to 448), top = 448: relative steps of 2^-4 .. 2^-3
+ *   VEGAS_QUANT_INT8   codes are signed integers, top = 127: steps of a / 127
+ * A row of a < 2^-110 is stored as zeros with scale 0; one that holds an infinity or a NaN with scale NaN and zero codes (it
+ * reads back as NaN; attention over it is unspecified).  Codes of appended rows are always finite.
+ *   scales   fp32 [num_pages16, H_kv, 2, 16]   of physical 16-token page, KV head, K (0) or V (1), slot; where page_size is
+ *            smaller, token slot s of the pool is page s / 16, slot s % 16, and num_pages counts the smaller pages
+ * ------------------------------------------------------------------------------------------------------------------- */
+enum { VEGAS_QUANT_E4M3 = 0, VEGAS_QUANT_INT8 = 1 };
+
+typedef struct vegas_quant {
+  void* k;            /* codes, one byte per element */
+  void* v;
+  float* scales;
+  int32_t format;     /* VEGAS_QUANT_* */
+  int32_t reserved;   /* must be 0 */
+} vegas_quant;
+
+/* Rotary positions: the first rot_dim dims of a head are rot_dim / 2 pairs, pair i of a token at position p is turned by
+ * the angle p * inv_freq[i] and multiplied by `magnitude`: (x, y) -> m (x cos - y sin, x sin + y cos).  The other dims pass
+ * through.  Angles are formed in 64 bits, so far positions keep theirs. */
+enum {
+  VEGAS_ROPE_HALF = 0,         /* pair i = dims i and i + rot_dim / 2 */
+  VEGAS_ROPE_INTERLEAVED = 1   /* pair i = dims 2 i and 2 i + 1 */
+};
+typedef struct vegas_rope {
+  const double* inv_freq;   /* DEVICE, [rot_dim / 2] radians per position */
+  float magnitude;
+  int32_t rot_dim;          /* a multiple of 16 (VEGAS_ERR_UNSUPPORTED otherwise), at most head_dim */
+  int32_t layout;           /* VEGAS_ROPE_* */
+  int32_t reserved;         /* must be 0 */
+} vegas_rope;
+
+/* Frequencies scaled for contexts `factor` times the original length. */
+enum {
+  VEGAS_ROPE_SCALE_NONE = 0,   /* base^(-2 i / rot_dim) */
+  VEGAS_ROPE_SCALE_LINEAR = 1, /* position interpolation: divided by factor */
+  VEGAS_ROPE_SCALE_NTK = 2,    /* base * factor^(rot_dim / (rot_dim - 2)): the slowest pair interpolated, the fastest kept */
+  VEGAS_ROPE_SCALE_YARN = 3    /* YaRN: pairs of more than beta_fast turns over original_len kept, of fewer than beta_slow
+                                  interpolated, a ramp between; magnitude 0.1 ln(factor) + 1 */
+};
+/* Host function: writes rot_dim / 2 doubles (HOST memory; the caller copies them to the device once) and the magnitude.
+ * factor, original_len and the betas (usually 32 and 1) are read by the scalings that use them.  rot_dim: any even number. */
+int vegas_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, int64_t original_len,
+                           double beta_fast, double beta_slow, double* inv_freq, float* magnitude);
+
+/*
+ * Rotary positions of the heads of a tensor (queries, keys, or both as one projection left them).
+ *   x, out       bf16 [num_tokens, num_heads, head_dim], strides between tokens and heads in elements (multiples of 8);
+ *                out == x with the same strides rotates in place, otherwise they must not overlap
+ *   positions    int32 [num_tokens]
+ * head_dim 128 or 64.  num_tokens == 0 does nothing.  One launch; no workspace.
+ */
+int vegas_rotate(const vegas_rope* rope, int32_t head_dim, int64_t num_tokens, int32_t num_heads, const int32_t* positions,
+                 const void* x, int64_t x_token_stride, int64_t x_head_stride, void* out, int64_t out_token_stride,
+                 int64_t out_head_stride, void* hip_stream);
+
+/* New tokens of every sequence of a batch, for vegas_append_quant. */
+typedef struct vegas_new_tokens {
+  const void* k;               /* bf16 [B, num_new, H_kv, D]; H_kv * D consecutive elements per token */
+  const void* v;
+  const void* q;               /* bf16 [B, num_new, H_q, D], or NULL: rotated into q_out in the same launch (needs `rope`) */
+  void* q_out;                 /* NULL exactly if q is; may be q itself (same stride) */
+  const int32_t* new_lens;     /* DEVICE int32 [B]: how many of its num_new rows sequence b has (clamped to 0 .. num_new; rows
+                                  past them are padding: not read, q_out not written), or NULL: all */
+  int64_t kv_token_stride;     /* elements between the tokens of k and of v (a multiple of 8; 0: H_kv * D); a sequence's rows follow */
+  int64_t q_token_stride;      /* the last sequence's.  Likewise for q and q_out (0: H_q * D) */
+  int64_t q_out_token_stride;
+  int32_t num_new;             /* at most 2^24 */
+  int32_t reserved;            /* must be 0 */
+} vegas_new_tokens;
+
+/*
+ * vegas_append_kv for an 8-bit cache: token t of sequence b is stored at position seq_lens[b] + t, its keys rotated for that
+ * position first (rope NULL: keys are stored as they come), and quantised from the fp32 result.
+ *   block_table, seq_lens   as for vegas_append_kv
+ *   seq_lens_out            int32 [B]: the lengths after the append.  seq_lens itself, or an array apart from it (prompts of many tokens
+ *                           then take one launch instead of two)
+ *   sel_table, sel_seq_lens, sel_page_size   the selection to grow by the new tokens, as for vegas_append_kv_extend; or NULL
+ * A sequence without room for its tokens (min(max_seq_len, 16 * max_blocks)) takes nothing: cache, selection and its rows of q_out
+ * are left alone and the length after is the length before.  No workspace.  desc->page_size is 16.
+ */
+int vegas_append_quant(const vegas_desc* desc, const vegas_quant* cache, const vegas_rope* rope, const vegas_new_tokens* tokens,
+                       const int32_t* block_table, const int32_t* seq_lens, int32_t* seq_lens_out, int32_t* sel_table,
+                       int32_t* sel_seq_lens, int32_t sel_page_size, void* hip_stream);
+
+/*
+ * Tokens of an 8-bit cache back as bf16 (code * scale, rounded once): token first[b] + t of sequence b's page list to row t.
+ *   table      int32 [B, max_sel_blocks]     page list of desc->page_size (1, 2, 4, 8, 16) tokens per page: a selection, or a block
+ *                                            table (with max_sel_blocks its row stride)
+ *   lens       int32 [B]                     tokens the list covers, at most max_seq_len
+ *   first      int32 [B] or NULL (0)         negative values count as 0
+ *   k_out, v_out  bf16 [B, num_tokens, H_kv, D]   rows past a list's end are left as they are
+ */
+int vegas_read_quant(const vegas_desc* desc, const vegas_quant* cache, const int32_t* table, const int32_t* lens,
+                     const int32_t* first, int32_t num_tokens, void* k_out, void* v_out, void* hip_stream);
+
+/* Bytes of device scratch that the two attention calls below may need for this descriptor (vegas_workspace_bytes is for the others).
+ * Pure host function; returns 0 if the descriptor is invalid. */
+size_t vegas_quant_workspace_bytes(const vegas_desc* desc);
+
+/*
+ * vegas_verify_attention over an 8-bit cache: the same arguments and outputs, with the values that the codes stand for as K
+ * and V; `workspace` is of at least vegas_quant_workspace_bytes(desc) bytes.  VEGAS_ERR_UNSUPPORTED for a local mask (desc->window) and for score_metric VEGAS_METRIC_TOKEN_LOGITS when
+ * collecting; a caller's kv_chunk_tokens is refused where the page scores of one chunk do not fit a workgroup (with 128 rows
+ * from 10000 tokens on).
+ */
+int vegas_verify_attention_quant(const vegas_desc* desc, const vegas_quant* cache, const void* q, const int32_t* block_table,
+                                 const int32_t* seq_lens, void* out, float* block_scores, void* workspace,
+                                 size_t workspace_bytes, void* hip_stream);
+
+/*
+ * vegas_draft_attention over an 8-bit cache: attention of one new token per sequence over a page list of 1, 2, 4, 8 or 16 tokens
+ * per page, split over the list's length and joined.  With a block table for a list (max_sel_blocks its row stride, max_seq_len the
+ * longest sequence) it is a decoding step of full attention.  `workspace`: at least vegas_quant_workspace_bytes(desc) bytes.
+ */
+int vegas_draft_attention_quant(const vegas_desc* desc, const vegas_quant* cache, const void* q, const int32_t* sel_table,
+                                const int32_t* sel_seq_lens, void* out, void* workspace, size_t workspace_bytes,
+                                void* hip_stream);
 
 /*
  * Profiling aids, not part of the method: the same calls restricted to some of their kernels.

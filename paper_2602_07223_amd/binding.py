@@ -38,9 +38,21 @@ CHECK_SHORTER_THAN_QUERIES = 8
 STAGE_STREAM = 1
 STAGE_MERGE = 2
 
+QUANT_E4M3 = 0
+QUANT_INT8 = 1
+
+ROPE_HALF = 0
+ROPE_INTERLEAVED = 1
+ROPE_SCALE_NONE = 0
+ROPE_SCALE_LINEAR = 1
+ROPE_SCALE_NTK = 2
+ROPE_SCALE_YARN = 3
+
 EXPORTS = ("vegas_init", "vegas_workspace_bytes", "vegas_verify_attention", "vegas_select_blocks",
            "vegas_select_tokens", "vegas_append_kv", "vegas_append_kv_extend", "vegas_extend_selection", "vegas_draft_attention",
            "vegas_draft_step", "vegas_draft_attention_static", "vegas_static_scratch_bytes",
+           "vegas_rope_frequencies", "vegas_rotate", "vegas_append_quant", "vegas_read_quant", "vegas_quant_workspace_bytes",
+           "vegas_verify_attention_quant", "vegas_draft_attention_quant",
            "vegas_debug_verify_attention_stages", "vegas_debug_draft_attention_stages", "vegas_debug_stream_read",
            "vegas_debug_check_tables", "vegas_debug_set_timeline", "vegas_debug_verify_waves", "vegas_strerror")
 
@@ -69,6 +81,25 @@ class VegasDesc(ctypes.Structure):
         ("kv_token_stride", ctypes.c_int64),
         ("kv_head_stride", ctypes.c_int64),
     ]
+
+
+class VegasQuant(ctypes.Structure):
+    """Mirror of ``vegas_quant`` (make_quant keeps the tensors it was made from in ``tensors``)."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("format", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class VegasRope(ctypes.Structure):
+    """Mirror of ``vegas_rope``."""
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("magnitude", ctypes.c_float), ("rot_dim", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class VegasNewTokens(ctypes.Structure):
+    """Mirror of ``vegas_new_tokens``."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q", ctypes.c_void_p), ("q_out", ctypes.c_void_p),
+                ("new_lens", ctypes.c_void_p), ("kv_token_stride", ctypes.c_int64), ("q_token_stride", ctypes.c_int64),
+                ("q_out_token_stride", ctypes.c_int64), ("num_new", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class VegasError(RuntimeError):
@@ -129,6 +160,23 @@ def load_library(path: Optional[str] = None):
     lib.vegas_debug_set_timeline.argtypes = [P, ctypes.c_size_t]
     lib.vegas_debug_verify_waves.restype = ctypes.c_int
     lib.vegas_debug_verify_waves.argtypes = [D]
+    Q, R, N = ctypes.POINTER(VegasQuant), ctypes.POINTER(VegasRope), ctypes.POINTER(VegasNewTokens)
+    lib.vegas_rope_frequencies.restype = ctypes.c_int
+    lib.vegas_rope_frequencies.argtypes = [ctypes.c_int32, ctypes.c_double, ctypes.c_int32, ctypes.c_double, ctypes.c_int64,
+                                           ctypes.c_double, ctypes.c_double, P, P]
+    lib.vegas_rotate.restype = ctypes.c_int
+    lib.vegas_rotate.argtypes = [R, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, P, P, ctypes.c_int64, ctypes.c_int64, P,
+                                 ctypes.c_int64, ctypes.c_int64, P]
+    lib.vegas_append_quant.restype = ctypes.c_int
+    lib.vegas_append_quant.argtypes = [D, Q, R, N, P, P, P, P, P, ctypes.c_int32, P]
+    lib.vegas_read_quant.restype = ctypes.c_int
+    lib.vegas_read_quant.argtypes = [D, Q, P, P, P, ctypes.c_int32, P, P, P]
+    lib.vegas_quant_workspace_bytes.restype = ctypes.c_size_t
+    lib.vegas_quant_workspace_bytes.argtypes = [D]
+    lib.vegas_verify_attention_quant.restype = ctypes.c_int
+    lib.vegas_verify_attention_quant.argtypes = [D, Q, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.vegas_draft_attention_quant.restype = ctypes.c_int
+    lib.vegas_draft_attention_quant.argtypes = [D, Q, P, P, P, P, P, ctypes.c_size_t, P]
     lib.vegas_strerror.restype = ctypes.c_char_p
     lib.vegas_strerror.argtypes = [ctypes.c_int]
     _lib = lib
@@ -459,6 +507,177 @@ def vegas_draft_step(cache_desc: VegasDesc, desc: VegasDesc, q, k_new, v_new, bl
         out_at, workspace_at, wb, stream_at)
     if rc != VEGAS_OK:
         raise VegasError(rc, "vegas_draft_step")
+
+
+# ---------------------------------------------------------------------------------------------
+# 8-bit K/V cache and rotary positions
+# ---------------------------------------------------------------------------------------------
+
+def quant_extent_bytes(desc: VegasDesc) -> int:
+    """Bytes the codes of K (or V) must span: cache_extent_bytes with elements of one byte."""
+    return cache_extent_bytes(desc) // 2
+
+
+def quant_scales_bytes(desc: VegasDesc) -> int:
+    """Bytes of the scales of a cache with desc.num_pages pages of desc.page_size tokens."""
+    pages16 = -(-int(desc.num_pages) * desc.page_size // 16)
+    return pages16 * desc.num_kv_heads * 32 * 4
+
+
+def make_quant(k, v, scales, fmt: int) -> VegasQuant:
+    """Handle of an 8-bit cache: code tensors, scales and format (QUANT_*).  Keeps the tensors alive."""
+    c = VegasQuant(_ptr(k), _ptr(v), _ptr(scales), fmt, 0)
+    c.tensors = (k, v, scales)
+    return c
+
+
+def _quant_fits(where: str, desc: VegasDesc, cache: VegasQuant) -> None:
+    k, v, scales = cache.tensors
+    if isinstance(k, int):
+        return
+    _fits(where, "k", k, quant_extent_bytes(desc))
+    _fits(where, "v", v, quant_extent_bytes(desc))
+    _fits(where, "scales", scales, quant_scales_bytes(desc))
+
+
+def vegas_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROPE_SCALE_NONE, factor: float = 1.0,
+                           original_len: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """(radians per position of each pair: a list of rot_dim / 2 floats, magnitude); host arithmetic."""
+    freq, magnitude = (ctypes.c_double * max(int(rot_dim) // 2, 1))(), ctypes.c_float()
+    rc = (_lib or load_library()).vegas_rope_frequencies(int(rot_dim), float(base), int(scaling), float(factor), int(original_len),
+                                                         float(beta_fast), float(beta_slow), freq, _byref(magnitude))
+    if rc != VEGAS_OK:
+        raise VegasError(rc, "vegas_rope_frequencies")
+    return list(freq)[:rot_dim // 2], float(magnitude.value)
+
+
+def make_rope(inv_freq, rot_dim: int, layout: int = ROPE_HALF, magnitude: float = 1.0) -> VegasRope:
+    """inv_freq: float64 tensor [rot_dim / 2] on the device (kept alive)."""
+    if inv_freq is not None and not isinstance(inv_freq, int):
+        if inv_freq.element_size() != 8 or not inv_freq.is_contiguous():
+            raise ValueError("make_rope: inv_freq is a contiguous float64 tensor")
+        _fits("make_rope", "inv_freq", inv_freq, rot_dim // 2 * 8)
+    r = VegasRope(_ptr(inv_freq), float(magnitude), rot_dim, layout, 0)
+    r.tensors = (inv_freq,)
+    return r
+
+
+def _rows_bytes(rows: int, stride: int, width: int) -> int:
+    """Bytes that `rows` rows of `width` bf16 elements span, `stride` elements apart."""
+    return 2 * ((rows - 1) * stride + width) if rows > 0 else 0
+
+
+def vegas_rotate(rope: VegasRope, head_dim: int, num_tokens: int, num_heads: int, positions, x, out, stream=None,
+                 x_strides=None, out_strides=None) -> None:
+    """x, out: bf16 [num_tokens, num_heads, head_dim]; strides (token, head) in elements, by default the tensors' own (contiguous
+    for raw addresses)."""
+    xs, os_ = x_strides, out_strides
+    if xs is None:
+        xs = (num_heads * head_dim, head_dim) if isinstance(x, int) else (x.stride(-3), x.stride(-2))
+    if os_ is None:
+        os_ = (num_heads * head_dim, head_dim) if isinstance(out, int) else (out.stride(-3), out.stride(-2))
+    x_at, out_at, positions_at = x, out, positions
+    if not (isinstance(x, int) and isinstance(out, int)):
+        width = (num_heads - 1) * xs[1] + head_dim
+        x_at = _fits("vegas_rotate", "x", x, _rows_bytes(num_tokens, xs[0], width))
+        out_at = _fits("vegas_rotate", "out", out, _rows_bytes(num_tokens, os_[0], (num_heads - 1) * os_[1] + head_dim))
+        positions_at = _fits("vegas_rotate", "positions", positions, num_tokens * 4)
+    rc = (_lib or load_library()).vegas_rotate(_byref(rope) if rope is not None else None, int(head_dim), int(num_tokens), int(num_heads), _ptr(positions_at), _ptr(x_at),
+                                               xs[0], xs[1], _ptr(out_at), os_[0], os_[1], _stream(stream))
+    if rc != VEGAS_OK:
+        raise VegasError(rc, "vegas_rotate")
+
+
+def make_new_tokens(k, v, num_new: int, *, q=None, q_out=None, new_lens=None, kv_token_stride: int = 0, q_token_stride: int = 0,
+                    q_out_token_stride: int = 0) -> VegasNewTokens:
+    """New rows of a batch for vegas_append_quant (0: contiguous rows).  Keeps the tensors alive."""
+    n = VegasNewTokens(_ptr(k), _ptr(v), _ptr(q), _ptr(q_out), _ptr(new_lens), kv_token_stride, q_token_stride, q_out_token_stride, num_new, 0)
+    n.tensors = (k, v, q, q_out, new_lens)
+    return n
+
+
+def vegas_append_quant(desc: VegasDesc, cache: VegasQuant, rope: Optional[VegasRope], tokens: VegasNewTokens, block_table, seq_lens,
+                       seq_lens_out, sel_table=None, sel_seq_lens=None, sel_page_size: int = 16, stream=None) -> None:
+    block_table_at, seq_lens_at, seq_lens_out_at, sel_table_at, sel_seq_lens_at = block_table, seq_lens, seq_lens_out, sel_table, sel_seq_lens
+    if not (isinstance(block_table, int) and isinstance(seq_lens, int)):
+        d, where = desc, "vegas_append_quant"
+        _quant_fits(where, d, cache)
+        k, v, q, q_out, new_lens = tokens.tensors
+        rows, kv_row, q_row = d.batch * tokens.num_new, d.num_kv_heads * d.head_dim, d.num_q_heads * d.head_dim
+        for name, x, stride, width in (("k", k, tokens.kv_token_stride, kv_row), ("v", v, tokens.kv_token_stride, kv_row),
+                                       ("q", q, tokens.q_token_stride, q_row), ("q_out", q_out, tokens.q_out_token_stride, q_row)):
+            _fits(where, name, x, _rows_bytes(rows, stride or width, width))
+        _fits(where, "new_lens", new_lens, d.batch * 4)
+        block_table_at = _fits(where, "block_table", block_table, d.batch * d.max_blocks * 4)
+        seq_lens_at = _fits(where, "seq_lens", seq_lens, d.batch * 4)
+        seq_lens_out_at = _fits(where, "seq_lens_out", seq_lens_out, d.batch * 4)
+        sel_table_at = _fits(where, "sel_table", sel_table, d.batch * d.max_sel_blocks * 4)
+        sel_seq_lens_at = _fits(where, "sel_seq_lens", sel_seq_lens, d.batch * 4)
+    rc = (_lib or load_library()).vegas_append_quant(
+        _byref(desc), _byref(cache), _byref(rope) if rope is not None else None, _byref(tokens), _ptr(block_table_at), _ptr(seq_lens_at),
+        _ptr(seq_lens_out_at), _ptr(sel_table_at), _ptr(sel_seq_lens_at), int(sel_page_size), _stream(stream))
+    if rc != VEGAS_OK:
+        raise VegasError(rc, "vegas_append_quant")
+
+
+def vegas_read_quant(desc: VegasDesc, cache: VegasQuant, table, lens, first, num_tokens: int, k_out, v_out, stream=None) -> None:
+    table_at, lens_at, first_at, k_out_at, v_out_at = table, lens, first, k_out, v_out
+    if not (isinstance(table, int) and isinstance(k_out, int)):
+        d, where = desc, "vegas_read_quant"
+        _quant_fits(where, d, cache)
+        rows = d.batch * int(num_tokens) * d.num_kv_heads * d.head_dim * 2
+        table_at = _fits(where, "table", table, d.batch * d.max_sel_blocks * 4)
+        lens_at = _fits(where, "lens", lens, d.batch * 4)
+        first_at = _fits(where, "first", first, d.batch * 4)
+        k_out_at = _fits(where, "k_out", k_out, rows)
+        v_out_at = _fits(where, "v_out", v_out, rows)
+    rc = (_lib or load_library()).vegas_read_quant(_byref(desc), _byref(cache), _ptr(table_at), _ptr(lens_at), _ptr(first_at), int(num_tokens),
+                                                   _ptr(k_out_at), _ptr(v_out_at), _stream(stream))
+    if rc != VEGAS_OK:
+        raise VegasError(rc, "vegas_read_quant")
+
+
+def vegas_quant_workspace_bytes(desc: VegasDesc) -> int:
+    return int((_lib or load_library()).vegas_quant_workspace_bytes(_byref(desc)))
+
+
+def vegas_verify_attention_quant(desc: VegasDesc, cache: VegasQuant, q, block_table, seq_lens, out, block_scores, workspace,
+                                 stream=None, workspace_bytes: Optional[int] = None) -> None:
+    wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
+    q_at, block_table_at, seq_lens_at, out_at, block_scores_at = q, block_table, seq_lens, out, block_scores
+    if not (isinstance(q, int) and isinstance(block_table, int)):
+        d, where = desc, "vegas_verify_attention_quant"
+        _quant_fits(where, d, cache)
+        rows = d.batch * d.num_queries * d.num_q_heads * d.head_dim * 2
+        q_at = _fits(where, "q", q, rows)
+        out_at = _fits(where, "out", out, rows)
+        block_table_at = _fits(where, "block_table", block_table, d.batch * d.max_blocks * 4)
+        seq_lens_at = _fits(where, "seq_lens", seq_lens, d.batch * 4)
+        if d.collect_rows != COLLECT_NONE:
+            block_scores_at = _fits(where, "block_scores", block_scores, d.batch * d.max_blocks * 4)
+    rc = (_lib or load_library()).vegas_verify_attention_quant(
+        _byref(desc), _byref(cache), _ptr(q_at), _ptr(block_table_at), _ptr(seq_lens_at), _ptr(out_at), _ptr(block_scores_at), _ptr(workspace),
+        wb, _stream(stream))
+    if rc != VEGAS_OK:
+        raise VegasError(rc, "vegas_verify_attention_quant")
+
+
+def vegas_draft_attention_quant(desc: VegasDesc, cache: VegasQuant, q, sel_table, sel_seq_lens, out, workspace, stream=None,
+                                workspace_bytes: Optional[int] = None) -> None:
+    wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
+    q_at, sel_table_at, sel_seq_lens_at, out_at = q, sel_table, sel_seq_lens, out
+    if not (isinstance(q, int) and isinstance(sel_table, int)):
+        d, where = desc, "vegas_draft_attention_quant"
+        _quant_fits(where, d, cache)
+        rows = d.batch * d.num_q_heads * d.head_dim * 2
+        q_at = _fits(where, "q", q, rows)
+        out_at = _fits(where, "out", out, rows)
+        sel_table_at = _fits(where, "sel_table", sel_table, d.batch * d.max_sel_blocks * 4)
+        sel_seq_lens_at = _fits(where, "sel_seq_lens", sel_seq_lens, d.batch * 4)
+    rc = (_lib or load_library()).vegas_draft_attention_quant(_byref(desc), _byref(cache), _ptr(q_at), _ptr(sel_table_at), _ptr(sel_seq_lens_at), _ptr(out_at),
+                                                              _ptr(workspace), wb, _stream(stream))
+    if rc != VEGAS_OK:
+        raise VegasError(rc, "vegas_draft_attention_quant")
 
 
 def vegas_static_scratch_bytes() -> int:

@@ -1,0 +1,402 @@
+// Around an 8-bit K/V cache: rotary positions, quantising new K/V rows into the cache, reading tokens back as bf16.
+//
+// Format.  A row is one token's K or V of one KV head, x[0 .. D).  With a = max |x| it is stored as D one-byte codes
+// round(x * (top * (1 / a))) and one fp32 scale a * (1 / top); top is the largest code, 448 (e4m3) or 127 (int8).  A row of a < 2^-110
+// is stored as zeros with scale 0 (top / a would leave the range of fp32); a row that holds an infinity or a NaN has scale NaN and
+// zero codes: codes are finite always, so a masked token of any content cannot reach a matrix product.  The codes lie as
+// the bf16 caches do ([page, slot, KV head, dim], strides of the caller's), the scales as [page, KV head, K or V, slot], so that the
+// attention kernels read a page's 2 x 16 scales of their head as one 128-byte line.
+//
+// Rotary positions.  Pair i of a head's first `rot` dims is turned by angle p f_i.  Angles are formed and reduced to a
+// fraction of a turn in 64 bits (32 lose 0.01 rad at 10^5 positions), sine and cosine and the rotation are 32-bit.
+//
+// All three kernels are elementwise passes: what bounds a large call is memory, a small one its launch and two dependent
+// round trips (the length or position, then the rows or page).  A lane has 16 elements of a row, 8 of each half of its pairs.
+#pragma once
+#include "select_blocks.hpp"
+#include "vegas_common.hpp"
+
+namespace vegas {
+
+constexpr int kE4m3 = 0, kInt8 = 1;           // VEGAS_QUANT_*
+constexpr int kRopeHalf = 0;                  // VEGAS_ROPE_HALF (1: interleaved)
+constexpr int kUnit = 16;                     // elements of a row that one lane has
+
+struct RopeParams {
+  const double* inv_freq;   // [rot / 2] radians per position
+  float magnitude;
+  int32_t rot, layout;
+};
+
+struct RotateParams {
+  RopeParams rope;
+  const int32_t* positions; // [N]
+  const uint16_t* x;        // bf16 [N, H, D]
+  uint16_t* out;
+  int64_t x_token, x_head, out_token, out_head;      // strides
+  int32_t N, H;
+  int32_t steps;            // steps of 64 / (D / 16) heads that one wave takes
+};
+
+struct QuantAppendParams {
+  RopeParams rope;          // inv_freq == nullptr: no rotation
+  const uint16_t* k_new;    // bf16 [B, T, Hkv, D]
+  const uint16_t* v_new;
+  const uint16_t* q;        // or nullptr; bf16 [B, T, Hq, D]
+  uint16_t* q_out;
+  const int32_t* new_lens;  // or nullptr
+  int64_t kv_token, q_token, q_out_token;            // strides between tokens
+  uint8_t* k_cache;
+  uint8_t* v_cache;
+  float* scales;
+  const int32_t* block_table;
+  const int32_t* seq_lens;
+  int32_t* seq_lens_out;
+  int32_t T, Hkv, Hq, max_blocks, max_tokens;
+  int32_t tokens, steps;    // of a workgroup; of a wave and token
+  int64_t page_stride, token_stride, head_stride, num_pages;
+  ExtendParams grow;        // sel_table != nullptr: the selection grows by the same tokens
+};
+
+struct QuantReadParams {
+  const uint8_t* k_cache;
+  const uint8_t* v_cache;
+  const float* scales;
+  const int32_t* table;     // [B, table_stride]
+  const int32_t* lens;
+  const int32_t* first;     // or nullptr
+  uint16_t* k_out;          // bf16 [B, T, Hkv, D]
+  uint16_t* v_out;
+  int32_t T, Hkv, table_stride, max_tokens, page_shift;
+  int64_t page_stride, token_stride, head_stride, num_pages;
+};
+
+// ---------------------------------------------------------------------------------------------------------- rotation
+
+// (cos, sin) * magnitude of position pos and frequencies 8 u .. 8 u + 7 (u: this lane's unit): lane i works out pair i, the
+// wave shares them through its 64 pairs of LDS.
+__device__ __forceinline__ void unit_angles(const RopeParams& rope, double freq, int pos, f32x2* lds, int u, f32x2 (&cs)[8]) {
+  const int lane = threadIdx.x & 63;
+  const double turns = static_cast<double>(pos) * freq * 0.15915494309189533577;   // 1 / (2 pi)
+  const float part = static_cast<float>(turns - __builtin_rint(turns));             // exact difference, in [-1/2, 1/2]
+  float s, c;
+  sincospif(2.0f * part, &s, &c);
+  wave_lds_fence();                           // (the last token's pairs have been read)
+  lds[lane] = f32x2{c * rope.magnitude, s * rope.magnitude};
+  wave_lds_fence();
+  const f32x4* at = reinterpret_cast<const f32x4*>(lds + 8 * min(u, 7));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const f32x4 two = at[i];
+    cs[2 * i] = f32x2{two[0], two[1]};
+    cs[2 * i + 1] = f32x2{two[2], two[3]};
+  }
+}
+__device__ __forceinline__ double lane_frequency(const RopeParams& rope) {
+  const int lane = threadIdx.x & 63;
+  return lane < (rope.rot >> 1) ? rope.inv_freq[lane] : 0.0;
+}
+
+// Where the two eights of this lane's unit lie in the row.
+struct UnitAt {
+  int a, b;
+  bool turned;
+};
+__device__ __forceinline__ UnitAt unit_at(const RopeParams& rope, bool rotates, int u) {
+  UnitAt at;
+  at.turned = rotates && u < (rope.rot >> 4);
+  const bool apart = at.turned && rope.layout == kRopeHalf;
+  at.a = apart ? 8 * u : 16 * u;
+  at.b = apart ? (rope.rot >> 1) + 8 * u : 16 * u + 8;
+  return at;
+}
+__device__ __forceinline__ void widen(const u32x4& raw, float* x) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(raw[e] << 16);
+    x[2 * e + 1] = __uint_as_float(raw[e] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ u32x4 narrow(const float* x) {     // to nearest even, NaN kept
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  u32x4 raw;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) raw[e] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(x[2 * e]), static_cast<__bf16>(x[2 * e + 1])});
+  return raw;
+}
+__device__ __forceinline__ void turn(float& a, float& b, const f32x2& cs) {
+  const float x = a, y = b;
+  a = x * cs[0] - y * cs[1];
+  b = x * cs[1] + y * cs[0];
+}
+__device__ __forceinline__ void turn_unit(const RopeParams& rope, float (&x)[kUnit], const f32x2 (&cs)[8]) {
+  if (rope.layout == kRopeHalf) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turn(x[i], x[8 + i], cs[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) turn(x[2 * i], x[2 * i + 1], cs[i]);
+  }
+}
+
+// A wave per token and `steps` steps of heads; four steps' requests leave together.
+template <int D>
+__global__ __launch_bounds__(256) void rotate_kernel(const RotateParams p) {
+  constexpr int LPR = D / kUnit, RPS = 64 / LPR, AHEAD = 4;     // lanes of a row, rows of a step
+  __shared__ f32x2 pairs[4][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int64_t tok = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+  if (tok >= p.N) return;
+  const int u = lane % LPR, row = lane / LPR;
+  const double freq = lane_frequency(p.rope);
+  const int pos = p.positions[tok];
+  const UnitAt at = unit_at(p.rope, true, u);
+  const uint16_t* const x = p.x + tok * p.x_token;
+  uint16_t* const out = p.out + tok * p.out_token;
+  const int s1 = min((static_cast<int>(blockIdx.y) + 1) * p.steps, (p.H + RPS - 1) / RPS);
+  f32x2 cs[8];
+  bool known = false;
+  for (int s0 = static_cast<int>(blockIdx.y) * p.steps; s0 < s1; s0 += AHEAD) {
+    u32x4 raw[AHEAD][2];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int h = (s0 + i) * RPS + row;
+      if (s0 + i < s1 && h < p.H) {
+        raw[i][0] = *reinterpret_cast<const u32x4*>(x + h * p.x_head + at.a);
+        raw[i][1] = *reinterpret_cast<const u32x4*>(x + h * p.x_head + at.b);
+      }
+    }
+    if (!known) unit_angles(p.rope, freq, pos, pairs[wave], u, cs);
+    known = true;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int h = (s0 + i) * RPS + row;
+      if (s0 + i < s1 && h < p.H) {
+        if (at.turned) {
+          float v[kUnit];
+          widen(raw[i][0], v);
+          widen(raw[i][1], v + 8);
+          turn_unit(p.rope, v, cs);
+          raw[i][0] = narrow(v);
+          raw[i][1] = narrow(v + 8);
+        }
+        *reinterpret_cast<u32x4*>(out + h * p.out_head + at.a) = raw[i][0];
+        *reinterpret_cast<u32x4*>(out + h * p.out_head + at.b) = raw[i][1];
+      }
+    }
+  }
+}
+
+// --------------------------------------------------------------------------------------------------------- quantising
+
+// Largest of the LPR (8 or 4) lanes of a row.
+template <int LPR>
+__device__ __forceinline__ uint32_t row_lanes_max(uint32_t x) {
+  auto with = [&](auto ctrl) {
+    const uint32_t y = __builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, 0xf, 0xf, true);
+    x = x > y ? x : y;
+  };
+  with(std::integral_constant<int, 0xB1>{});                     // quad_perm: lanes 1 apart, 2 apart
+  with(std::integral_constant<int, 0x4E>{});
+  if constexpr (LPR == 8) with(std::integral_constant<int, 0x141>{});   // row_half_mirror: the other four
+  return x;
+}
+
+// Codes (4 dwords) and scale of a row whose lanes have 16 elements each.
+template <int FMT, int LPR>
+__device__ __forceinline__ u32x4 quantise_unit(const float (&x)[kUnit], float& scale) {
+  constexpr float kTop = FMT == kE4m3 ? 448.f : 127.f;
+  constexpr float kTiny = 0x1p-110f;
+  uint32_t top = 0u;                          // (bit patterns: a NaN is larger than every number)
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) {
+    const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
+    top = top > a ? top : a;
+  }
+  const float a = __uint_as_float(row_lanes_max<LPR>(top));
+  const bool finite = __float_as_uint(a) < 0x7f800000u, live = finite && a >= kTiny;
+  // (One correctly rounded reciprocal, products otherwise, each rounded by itself: whoever computes these gets the same codes.)
+  const float inv = __fmul_rn(kTop, __frcp_rn(live ? a : 1.f));
+  scale = !finite ? __builtin_nanf("") : live ? __fmul_rn(a, 1.f / kTop) : 0.f;
+  u32x4 codes;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = x[4 * e + i] * inv;
+    uint32_t c;
+    if constexpr (FMT == kE4m3) {
+      int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+      c = static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true));
+    } else {
+      c = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c |= (static_cast<uint32_t>(static_cast<int>(__builtin_rintf(live ? y[i] : 0.f))) & 0xffu) << (8 * i);
+    }
+    codes[e] = live ? c : 0u;
+  }
+  return codes;
+}
+
+// New tokens of sequence blockIdx.z: a wave takes a token at a time, and of its steps (64 / (D / 16) heads of K, of V, of the
+// queries) those of its grid row.  The length is read by every wave; who stores the new one has to be last:
+//   IN_PLACE: one workgroup per sequence, a barrier between (few tokens); otherwise seq_lens_out is another array, or nullptr where
+//   a second launch (advance_lengths_kernel) stores it.
+template <int D, int FMT, bool IN_PLACE>
+__global__ __launch_bounds__(IN_PLACE ? 1024 : 256) void append_quant_kernel(const QuantAppendParams p) {
+  constexpr int LPR = D / kUnit, RPS = 64 / LPR, NW = IN_PLACE ? 16 : 4;
+  __shared__ f32x2 pairs[NW][64];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int b = blockIdx.z;
+  const int u = lane % LPR, row = lane / LPR;
+  const bool rotates = p.rope.inv_freq != nullptr;
+  const double freq = rotates ? lane_frequency(p.rope) : 0.0;
+  const int n = p.seq_lens[b];
+  int count = p.T;
+  if (p.new_lens) count = min(max(p.new_lens[b], 0), p.T);
+  if constexpr (IN_PLACE) __syncthreads();
+  const int64_t cap = min(static_cast<int64_t>(p.max_blocks) * kPage, static_cast<int64_t>(p.max_tokens));
+  if (n < 0 || static_cast<int64_t>(n) + count > cap) count = 0;      // no room: the sequence takes nothing
+  const int sk = (p.Hkv + RPS - 1) / RPS, all = 2 * sk + (p.q ? (p.Hq + RPS - 1) / RPS : 0);
+  const int32_t* const table = p.block_table + static_cast<int64_t>(b) * p.max_blocks;
+  const UnitAt turned = unit_at(p.rope, rotates, u), plain = unit_at(p.rope, false, u);
+
+  auto step = [&](int t, int s, int64_t page, const f32x2 (&cs)[8]) {
+    const int64_t token = static_cast<int64_t>(b) * p.T + t;
+    if (s >= 2 * sk) {                       // queries: rotated, bf16 again
+      const int h = (s - 2 * sk) * RPS + row;
+      if (h >= p.Hq) return;
+      const uint16_t* src = p.q + token * p.q_token + h * D;
+      uint16_t* dst = p.q_out + token * p.q_out_token + h * D;
+      u32x4 lo = *reinterpret_cast<const u32x4*>(src + turned.a), hi = *reinterpret_cast<const u32x4*>(src + turned.b);
+      if (turned.turned) {
+        float x[kUnit];
+        widen(lo, x);
+        widen(hi, x + 8);
+        turn_unit(p.rope, x, cs);
+        lo = narrow(x);
+        hi = narrow(x + 8);
+      }
+      *reinterpret_cast<u32x4*>(dst + turned.a) = lo;
+      *reinterpret_cast<u32x4*>(dst + turned.b) = hi;
+      return;
+    }
+    const bool is_v = s >= sk;
+    const int h = (s - (is_v ? sk : 0)) * RPS + row;
+    if (h >= p.Hkv) return;                  // (whole rows of lanes)
+    const UnitAt at = is_v ? plain : turned;
+    const uint16_t* src = (is_v ? p.v_new : p.k_new) + token * p.kv_token + h * D;
+    float x[kUnit];
+    widen(*reinterpret_cast<const u32x4*>(src + at.a), x);
+    widen(*reinterpret_cast<const u32x4*>(src + at.b), x + 8);
+    if (at.turned) turn_unit(p.rope, x, cs);
+    // (The rotated key is quantised from fp32: a bf16 in between would be a second rounding and save nothing.)
+    float scale;
+    const u32x4 codes = quantise_unit<FMT, LPR>(x, scale);
+    const int slot = (n + t) % kPage;
+    uint8_t* dst = (is_v ? p.v_cache : p.k_cache) + page * p.page_stride + slot * p.token_stride + h * p.head_stride;
+    *reinterpret_cast<u32x2*>(dst + at.a) = u32x2{codes[0], codes[1]};
+    *reinterpret_cast<u32x2*>(dst + at.b) = u32x2{codes[2], codes[3]};
+    if (u == 0) p.scales[((page * p.Hkv + h) * 2 + (is_v ? 1 : 0)) * kPage + slot] = scale;
+  };
+  auto token = [&](int t, int s0, int s1) {
+    int64_t page = table[(n + t) / kPage];
+    page = page < 0 ? 0 : (page >= p.num_pages ? p.num_pages - 1 : page);   // a corrupt table cannot fault
+    f32x2 cs[8];
+    if (rotates) unit_angles(p.rope, freq, n + t, pairs[wave], u, cs);
+    for (int s = s0; s < s1; ++s) step(t, s, page, cs);
+  };
+  if constexpr (IN_PLACE) {
+    for (int i = wave; i < count * all; i += NW) token(i / all, i % all, i % all + 1);
+  } else {
+    const int s0 = static_cast<int>(blockIdx.y) * p.steps;
+    const int t1 = min((static_cast<int>(blockIdx.x) + 1) * p.tokens, count);
+    for (int t = static_cast<int>(blockIdx.x) * p.tokens + wave; t < t1; t += NW) token(t, s0, min(s0 + p.steps, all));
+  }
+  if (threadIdx.x == 0 && (blockIdx.x | blockIdx.y) == 0 && p.seq_lens_out != nullptr) {
+    p.seq_lens_out[b] = n + count;
+    if (p.grow.sel_table != nullptr && count > 0) {
+      ExtendParams grow = p.grow;
+      grow.num_new = count;
+      extend_selection_row(grow, b, n + count);
+    }
+  }
+}
+
+// The lengths (and selections) behind an append of many tokens in place, one thread per sequence.
+__global__ void advance_lengths_kernel(const QuantAppendParams p, int32_t* seq_lens, int batch) {
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b >= batch) return;
+  const int n = seq_lens[b];
+  int count = p.T;
+  if (p.new_lens) count = min(max(p.new_lens[b], 0), p.T);
+  const int64_t cap = min(static_cast<int64_t>(p.max_blocks) * kPage, static_cast<int64_t>(p.max_tokens));
+  if (n < 0 || count == 0 || static_cast<int64_t>(n) + count > cap) return;
+  seq_lens[b] = n + count;
+  if (p.grow.sel_table != nullptr) {
+    ExtendParams grow = p.grow;
+    grow.num_new = count;
+    extend_selection_row(grow, b, n + count);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------- reading back
+
+// Eight codes as fp32.
+template <int FMT>
+__device__ __forceinline__ void widen_codes(const u32x2& w, float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if constexpr (FMT == kE4m3) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[e]), false);
+      const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(static_cast<int>(w[e]), true);
+      x[4 * e] = lo[0]; x[4 * e + 1] = lo[1]; x[4 * e + 2] = hi[0]; x[4 * e + 3] = hi[1];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * e + i] = static_cast<float>(static_cast<int8_t>(w[e] >> (8 * i)));
+    }
+  }
+}
+
+// A workgroup has 16 consecutive tokens of a sequence's list, a wave every fourth of them, a lane 8 elements of a row: it reads
+// 8 bytes of a token's codes and writes 16 of its output row, both without gaps between lanes (NHD).
+constexpr int kReadTokens = 16;
+template <int D, int FMT>
+__global__ __launch_bounds__(256) void read_quant_kernel(const QuantReadParams p) {
+  constexpr int LPR = D / 8;                 // lanes of a row
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int b = blockIdx.z;
+  int n = p.lens[b];
+  n = n < 0 ? 0 : (n > p.max_tokens ? p.max_tokens : n);
+  const int first = p.first ? max(p.first[b], 0) : 0;
+  const int t0 = static_cast<int>(blockIdx.x) * kReadTokens;
+  const int t1 = static_cast<int>(min(static_cast<int64_t>(min(t0 + kReadTokens, p.T)), static_cast<int64_t>(n) - first));
+  const int32_t* const table = p.table + static_cast<int64_t>(b) * p.table_stride;
+  for (int t = t0 + wave; t < t1; t += 4) {
+    const int pos = first + t;
+    int64_t page = table[pos >> p.page_shift];
+    page = page < 0 ? 0 : (page >= p.num_pages ? p.num_pages - 1 : page);
+    const int in_page = pos & ((1 << p.page_shift) - 1);
+    const int64_t slot = (page << p.page_shift) + in_page;             // of the pool
+    const int64_t at = page * p.page_stride + in_page * p.token_stride;
+    const int64_t out = (static_cast<int64_t>(b) * p.T + t) * p.Hkv * D;
+    const float* const scales = p.scales + (slot / kPage) * p.Hkv * 32 + slot % kPage;
+    for (int e = lane; e < p.Hkv * LPR; e += 64) {
+      const int h = e / LPR;
+      const int64_t src = at + h * p.head_stride + (e % LPR) * 8;
+      const u32x2 k = *reinterpret_cast<const u32x2*>(p.k_cache + src), v = *reinterpret_cast<const u32x2*>(p.v_cache + src);
+      const float ks = scales[h * 32], vs = scales[h * 32 + kPage];
+      float x[8];
+      widen_codes<FMT>(k, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= ks;
+      *reinterpret_cast<u32x4*>(p.k_out + out + e * 8) = narrow(x);
+      widen_codes<FMT>(v, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= vs;
+      *reinterpret_cast<u32x4*>(p.v_out + out + e * 8) = narrow(x);
+    }
+  }
+}
+
+}  // namespace vegas

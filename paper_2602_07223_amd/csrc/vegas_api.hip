@@ -14,10 +14,12 @@
 #include "attn_finalize.hpp"
 #include "attn_draft.hpp"
 #include "attn_pair.hpp"
+#include "attn_quant.hpp"
 #include "attn_split.hpp"
 #include "debug_kernels.hpp"
 #include "kv_append.hpp"
 #include "plan_rules.hpp"
+#include "quant_cache.hpp"
 #include "select_blocks.hpp"
 #include "select_tokens.hpp"
 #include "vegas_common.hpp"
@@ -501,6 +503,79 @@ int launch_combine(const vegas_desc* d, const SplitPlan& pl, const SplitParams& 
   return hipGetLastError() == hipSuccess ? VEGAS_OK : VEGAS_ERR_LAUNCH;
 }
 
+// An upper bound of the LDS that the page scores' roles lay out (at most 13 x rows + 262 floats of collected rows, up to Hkv R;
+// verify_finalize_kernel), by which a call of more than 2394 rows is refused.
+size_t finalize_lds(const vegas_desc* d, const SplitPlan& pl) {
+  const size_t hr = static_cast<size_t>(d->num_kv_heads) * pl.R;
+  return (hr + 256 + 16 * hr) * sizeof(float);
+}
+
+// Merge of a verification's chunk partials with its scores (page weights, or token sums of the logit metric) in one launch.
+int launch_finalize(const vegas_desc* desc, const SplitPlan& pl, const SplitParams& sp, bool logits, const int32_t* seq_lens, void* out,
+                    float* block_scores, hipStream_t st) {
+  FinalizeParams fp;
+  fp.part_o = sp.part_o;
+  fp.part_ml = sp.part_ml;
+  fp.page_lse = sp.page_lse;
+  fp.lens = seq_lens;
+  fp.out = static_cast<uint16_t*>(out);
+  fp.block_scores = block_scores;
+  fp.G = desc->num_queries; fp.g = sp.g; fp.R = pl.R; fp.Hq = sp.Hq; fp.Hkv = sp.Hkv;
+  fp.chunk_tokens = pl.chunk; fp.nsplit = pl.nsplit; fp.max_tokens = desc->max_seq_len;
+  fp.max_blocks = desc->max_blocks; fp.lse_pages = pl.lse_pages; fp.collect_rows = desc->collect_rows;
+  fp.Rc = pl.Rc;
+  fp.D = desc->head_dim;
+  fp.plan = sp.plan;
+  fp.slots_total = sp.slots_total;
+  const bool small = planned_merge_is_small(desc->batch, sp.Hkv * pl.R, fp.D);
+  const int rows_per_wg = (pl.balanced && !small ? 1024 : 256) / fp.D;   // merge workgroups: 256 threads, D per row, or D / 4
+  fp.nA = (sp.Hkv * pl.R + rows_per_wg - 1) / rows_per_wg;
+  const int nrows = (desc->collect_rows == VEGAS_COLLECT_ALL_ROWS) ? desc->num_queries
+                                                                   : (desc->num_queries > 1 ? 2 : 1);
+  fp.inv_norm = 1.0f / (static_cast<float>(nrows) * static_cast<float>(desc->num_q_heads));
+  // Every score workgroup (32 pages) rebuilds the row log-sum-exps from the (rows x chunks) table of
+  // (max, sum) pairs; giving a workgroup more pages to amortise that was measured slower.
+  int nB = (desc->max_blocks + 31) / 32;
+  size_t shm = finalize_lds(desc, pl);
+  fp.nC = 0;
+  fp.tok_norm = 0.f;
+  if (logits) {                                        // token sums instead of page scores: 1024 tokens per workgroup
+    fp.nC = static_cast<int>((static_cast<int64_t>(desc->max_blocks) * kPage + 1023) / 1024);
+    fp.tok_norm = desc->softmax_scale / (static_cast<float>(nrows) * static_cast<float>(desc->num_q_heads));
+    nB = fp.nC;
+    shm = 272 * sizeof(float);
+  }
+  if (shm > 160 * 1024) return VEGAS_ERR_UNSUPPORTED;
+  const dim3 fgrid(fp.nA + nB, desc->batch);
+  int rc = VEGAS_OK;
+  auto launch = [&](auto kern) -> int {
+    if (int lrc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), shm)) return lrc;
+    hipLaunchKernelGGL(kern, fgrid, dim3(256), shm, st, fp);
+    return VEGAS_OK;
+  };
+  if (logits) {
+    if (pl.balanced && small) rc = launch(verify_finalize_kernel<kFinPlannedSmall, 1>);
+    else if (pl.balanced) rc = launch(verify_finalize_kernel<kFinPlanned, 1>);
+    else if (pl.nsplit <= 16) rc = launch(verify_finalize_kernel<16, 1>);
+    else if (pl.nsplit <= 32) rc = launch(verify_finalize_kernel<32, 1>);
+    else if (pl.nsplit <= 64) rc = launch(verify_finalize_kernel<64, 1>);
+    else rc = launch(verify_finalize_kernel<0, 1>);
+  } else {
+    if (pl.balanced && small) rc = launch(verify_finalize_kernel<kFinPlannedSmall>);
+    else if (pl.balanced) rc = launch(verify_finalize_kernel<kFinPlanned>);
+    else if (finalize_is_wide(sp.Hkv * pl.Rc, desc->batch, pl.nsplit)) {
+      if (pl.nsplit <= 16) rc = launch(verify_finalize_kernel<16, 0, kFinWideRounds>);
+      else rc = launch(verify_finalize_kernel<32, 0, kFinWideRounds>);
+    } else if (pl.nsplit <= 16) rc = launch(verify_finalize_kernel<16>);
+    else if (pl.nsplit <= 32) rc = launch(verify_finalize_kernel<32>);
+    else if (pl.nsplit <= 64) rc = launch(verify_finalize_kernel<64>);
+    else rc = launch(verify_finalize_kernel<0>);
+  }
+  if (rc != VEGAS_OK) return rc;
+  if (hipGetLastError() != hipSuccess) return VEGAS_ERR_LAUNCH;
+  return VEGAS_OK;
+}
+
 // Scratch of vegas_draft_attention_static: the chunk partials of one draft call, in the library's own device image
 // instead of a caller's workspace.  Every device the library runs on holds its own copy of the array at its own
 // address until the process ends.  In host code the array's name is only a handle for hipGetSymbolAddress: the
@@ -530,6 +605,32 @@ int static_scratch_address(void** out) {
   known[dev] = ptr;
   *out = ptr;
   return VEGAS_OK;
+}
+
+// Waves of a workgroup over an 8-bit cache: verification fills a compute unit with one, draft calls put several side by side.
+constexpr int kQuantVerifyWaves = 8, kQuantDraftWaves = 4;
+
+// For vegas_init: every kernel of attn_quant.hpp.
+template <typename F>
+void for_each_quant_kernel(F one) {
+  auto rows = [&](auto dim, auto format, auto nt) {
+    constexpr int D = decltype(dim)::value, FMT = decltype(format)::value, NT = decltype(nt)::value;
+    if constexpr (NT <= kQuantDraftNT) {
+      one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, true, 0, false>);
+      one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, false, 0, false>);
+    }
+    one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 1, true>);
+    one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 0, true>);
+  };
+  auto formats = [&](auto dim, auto format) {
+    rows(dim, format, std::integral_constant<int, 1>{});
+    rows(dim, format, std::integral_constant<int, 2>{});
+    rows(dim, format, std::integral_constant<int, 3>{});
+  };
+  formats(std::integral_constant<int, 128>{}, std::integral_constant<int, kE4m3>{});
+  formats(std::integral_constant<int, 128>{}, std::integral_constant<int, kInt8>{});
+  formats(std::integral_constant<int, 64>{}, std::integral_constant<int, kE4m3>{});
+  formats(std::integral_constant<int, 64>{}, std::integral_constant<int, kInt8>{});
 }
 
 // Every kernel that is launched with dynamic LDS, for vegas_init: f(kernel address).
@@ -578,7 +679,169 @@ int for_each_lds_kernel(F f) {
   one(verify_finalize_kernel<kFinPlanned, 0>); one(verify_finalize_kernel<kFinPlanned, 1>);
   one(verify_finalize_kernel<kFinPlannedSmall, 0>); one(verify_finalize_kernel<kFinPlannedSmall, 1>);
   one(select_blocks_kernel<kSelectThreads>);
+  for_each_quant_kernel(one);
   return rc;
+}
+
+// ---- calls over an 8-bit cache (attn_quant.hpp, quant_cache.hpp)
+
+constexpr size_t kQuantLds = 150 * 1024;      // what a verification workgroup takes at most
+
+struct QuantPlan : SplitPlan {
+  int NT = 1;                        // 16-row tiles of a workgroup
+  size_t park = 0;                   // LDS in front of the queries
+  size_t lds = 0;
+};
+
+int plan_quant(const vegas_desc* d, int rows, bool collect, bool draft, QuantPlan* pl) {
+  if (rows > 128) return VEGAS_ERR_UNSUPPORTED;
+  const int num_cu = device_cu_count();
+  const int64_t heads = static_cast<int64_t>(d->batch) * d->num_kv_heads;
+  const int max_len = d->max_seq_len;
+  pl->R = rows;
+  // Row blocks: as many 16-row tiles as registers hold share a tile's loads and conversions, more rows are sibling workgroups.
+  const int tiles = (rows + 15) / 16;
+  const int most_tiles = draft ? kQuantDraftNT : kQuantVerifyNT;
+  pl->NB = (tiles + most_tiles - 1) / most_tiles;
+  pl->NT = (tiles + pl->NB - 1) / pl->NB;
+  pl->NW = draft ? kQuantDraftWaves : kQuantVerifyWaves;
+  const int unit = kTile * pl->NW;
+  const int block_rows = rows < 16 * pl->NT ? rows : 16 * pl->NT;
+  const size_t tail = quant_tail_bytes(pl->NW, pl->NT, d->head_dim);
+  const int64_t per_head = static_cast<int64_t>(d->num_kv_heads) * pl->NB;
+  const int whole = (max_len + unit - 1) / unit * unit;
+  int cap = 1 << 24;                 // tokens whose page log-sum-exps a workgroup can park
+  if (collect) {
+    cap = static_cast<int>((kQuantLds - tail) / (block_rows * sizeof(float))) * kPage / unit * unit;
+    if (cap > (1 << 24)) cap = 1 << 24;
+  }
+  pl->balanced = !draft && d->kv_chunk_tokens == 0 && d->batch >= 2 && d->batch <= 64 && max_len < (1 << 24) && per_head <= num_cu;
+  int chunk = d->kv_chunk_tokens;
+  if (chunk == 0) {
+    const int64_t columns = heads * pl->NB;
+    int64_t splits = static_cast<int64_t>(num_cu) * (draft ? 2 : 1) / columns;
+    if (splits < 1) splits = 1;
+    int64_t c = (max_len + splits - 1) / splits;
+    c = (c + unit - 1) / unit * unit;
+    const int64_t most = columns >= num_cu ? 2048 : 1 << 24;
+    if (c > most) c = most;
+    if (c > cap) c = cap;
+    chunk = static_cast<int>(c);
+  } else if (chunk > cap) {
+    return VEGAS_ERR_UNSUPPORTED;
+  }
+  const bool finish = draft && d->kv_chunk_tokens == 0 && max_len <= lone_workgroup_tokens(heads * pl->NB, num_cu, d->head_dim);
+  size_t slots = static_cast<size_t>(heads) * ((max_len + chunk - 1) / chunk);
+  if (finish) chunk = whole;
+  pl->chunk = chunk;
+  pl->nsplit = (max_len + chunk - 1) / chunk;
+  if (pl->balanced) {
+    pl->bp = batch_plan(num_cu, per_head, d->batch, max_len, unit, cap / unit, false, false, collect, d->head_dim);
+    pl->chunk = collect ? cap : unit;
+    slots = static_cast<size_t>(d->num_kv_heads) * pl->bp.JS;
+  }
+  pl->lse_pages = collect ? (max_len + kPage - 1) / kPage : 0;
+  pl->park = quant_park_bytes(pl->NW, block_rows, pl->chunk, collect, d->head_dim);
+  pl->lds = pl->park + tail;
+  if (pl->balanced && pl->bp.alone && pl->lds < kLoneLds) pl->lds = kLoneLds;
+  if (pl->lds > 160 * 1024) return VEGAS_ERR_UNSUPPORTED;
+  size_t off = 0;
+  pl->off_part_o = off;  off += align_up(slots * pl->R * d->head_dim * sizeof(float));
+  pl->off_part_ml = off; off += align_up(slots * pl->R * sizeof(float2));
+  pl->off_page_lse = off;
+  pl->Rc = collected_count(d->collect_rows, draft ? 1 : d->num_queries, d->num_q_heads / d->num_kv_heads);
+  off += align_up(static_cast<size_t>(heads) * pl->lse_pages * pl->Rc * sizeof(float));
+  pl->off_plan = off;
+  if (pl->balanced) off += align_up(static_cast<size_t>(d->batch) * sizeof(int2));
+  pl->total = off;
+  return VEGAS_OK;
+}
+
+// Bytes of a cache are its elements: rows are read 16 bytes at a time.
+int check_quant(const vegas_desc* d, const vegas_quant* c) {
+  if (!c || !c->k || !c->v || !c->scales) return VEGAS_ERR_NULL;
+  if (c->format != VEGAS_QUANT_E4M3 && c->format != VEGAS_QUANT_INT8) return VEGAS_ERR_UNSUPPORTED;
+  if (c->reserved != 0) return VEGAS_ERR_SHAPE;
+  if ((d->kv_head_stride % 16) || (d->kv_token_stride % 16) || (d->kv_page_stride % 16)) return VEGAS_ERR_ALIGN;
+  if (d->kv_token_stride > (1 << 26)) return VEGAS_ERR_UNSUPPORTED;       // (a page's offsets are 32-bit)
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->scales)) return VEGAS_ERR_ALIGN;
+  return VEGAS_OK;
+}
+
+int page_shift_of(int page_size) {
+  int shift = 0;
+  while ((1 << shift) < page_size) ++shift;
+  return shift;
+}
+
+// The grid that quant_stream_kernel reads its indices off: (chunk in a group of 8, KV head and row block, group and sequence).
+int quant_groups(const QuantPlan& pl) { return pl.balanced ? 1 : (pl.nsplit + 7) / 8; }
+dim3 quant_grid(const QuantPlan& pl, int kv_heads, int batch) {
+  const unsigned slots = pl.balanced ? pl.bp.JS : pl.nsplit;
+  return dim3(slots < 8 ? slots : 8, static_cast<unsigned>(kv_heads) * pl.NB,
+              pl.balanced ? (slots + 7) / 8 : static_cast<unsigned>(quant_groups(pl)) * batch);
+}
+// Does a dimension of it pass what a launch takes?
+bool exceeds_quant_grid(const vegas_desc* d, const QuantPlan& pl) {
+  return static_cast<int64_t>(d->num_kv_heads) * pl.NB > 65535 || static_cast<int64_t>(quant_groups(pl)) * d->batch > 65535 || pl.bp.JS > 8 * 65535;
+}
+
+template <int D, int FMT, int NT>
+int launch_quant_nt(const vegas_desc* d, const QuantPlan& pl, const SplitParams& sp, const QuantArgs& qa, bool draft, bool collect, hipStream_t st) {
+  const dim3 grid = quant_grid(pl, sp.Hkv, d->batch);
+  const dim3 block(pl.NW * 64);
+  if constexpr (NT <= kQuantDraftNT) {
+    if (draft && d->page_size != kPage) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, true, 0, false>, grid, block, pl.lds, st, sp, qa);
+    if (draft) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, false, 0, false>, grid, block, pl.lds, st, sp, qa);
+  }
+  if (collect) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 1, true>, grid, block, pl.lds, st, sp, qa);
+  return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 0, true>, grid, block, pl.lds, st, sp, qa);
+}
+template <int D, int FMT>
+int launch_quant_rows(const vegas_desc* d, const QuantPlan& pl, const SplitParams& sp, const QuantArgs& qa, bool draft, bool collect, hipStream_t st) {
+  switch (pl.NT) {
+    case 1: return launch_quant_nt<D, FMT, 1>(d, pl, sp, qa, draft, collect, st);
+    case 2: return launch_quant_nt<D, FMT, 2>(d, pl, sp, qa, draft, collect, st);
+    default: return launch_quant_nt<D, FMT, 3>(d, pl, sp, qa, draft, collect, st);
+  }
+}
+int launch_quant(const vegas_desc* d, const vegas_quant* c, const QuantPlan& pl, const SplitParams& sp, bool draft, bool collect, hipStream_t st) {
+  QuantArgs qa;
+  qa.scales = c->scales;
+  qa.page_shift = page_shift_of(d->page_size);
+  qa.park_bytes = static_cast<int32_t>(pl.park);
+  if (d->head_dim == 128)
+    return c->format == VEGAS_QUANT_E4M3 ? launch_quant_rows<128, kE4m3>(d, pl, sp, qa, draft, collect, st)
+                                         : launch_quant_rows<128, kInt8>(d, pl, sp, qa, draft, collect, st);
+  return c->format == VEGAS_QUANT_E4M3 ? launch_quant_rows<64, kE4m3>(d, pl, sp, qa, draft, collect, st)
+                                       : launch_quant_rows<64, kInt8>(d, pl, sp, qa, draft, collect, st);
+}
+
+// Steps that one wave of the rotating and the quantising kernel takes of a token's `all`: as many as leave 16 waves per compute unit, so that
+// a token's angles are worked out once where there are many tokens.
+int wave_steps(int64_t tokens, int all) {
+  const int64_t steps = tokens * all / (16 * static_cast<int64_t>(device_cu_count()));
+  return static_cast<int>(steps < 1 ? 1 : steps > all ? all : steps);
+}
+constexpr int kOneWorkgroupSteps = 64;       // of an append in place that one workgroup per sequence does
+
+int check_rope(const vegas_rope* r, int head_dim) {
+  if (!r) return VEGAS_ERR_NULL;
+  if (!r->inv_freq) return VEGAS_ERR_NULL;
+  if (r->layout != VEGAS_ROPE_HALF && r->layout != VEGAS_ROPE_INTERLEAVED) return VEGAS_ERR_UNSUPPORTED;
+  if (r->rot_dim <= 0 || r->rot_dim > head_dim) return VEGAS_ERR_SHAPE;
+  if (r->rot_dim % 16) return VEGAS_ERR_UNSUPPORTED;
+  if (r->reserved != 0 || !std::isfinite(r->magnitude)) return VEGAS_ERR_SHAPE;
+  if (reinterpret_cast<uintptr_t>(r->inv_freq) % alignof(double)) return VEGAS_ERR_ALIGN;
+  return VEGAS_OK;
+}
+RopeParams rope_params(const vegas_rope* r) {
+  RopeParams p;
+  p.inv_freq = r ? r->inv_freq : nullptr;
+  p.magnitude = r ? r->magnitude : 1.f;
+  p.rot = r ? r->rot_dim : 0;
+  p.layout = r ? r->layout : 0;
+  return p;
 }
 
 }  // namespace
@@ -656,69 +919,7 @@ static int verify_impl(const vegas_desc* desc, const void* q, const void* k_cach
   }
   if (!do_merge || direct) return VEGAS_OK;
   if (!collect) return launch_combine(desc, pl, sp, out, st);
-  FinalizeParams fp;
-  fp.part_o = sp.part_o;
-  fp.part_ml = sp.part_ml;
-  fp.page_lse = sp.page_lse;
-  fp.lens = seq_lens;
-  fp.out = static_cast<uint16_t*>(out);
-  fp.block_scores = block_scores;
-  fp.G = desc->num_queries; fp.g = sp.g; fp.R = pl.R; fp.Hq = sp.Hq; fp.Hkv = sp.Hkv;
-  fp.chunk_tokens = pl.chunk; fp.nsplit = pl.nsplit; fp.max_tokens = desc->max_seq_len;
-  fp.max_blocks = desc->max_blocks; fp.lse_pages = pl.lse_pages; fp.collect_rows = desc->collect_rows;
-  fp.Rc = pl.Rc;
-  fp.D = desc->head_dim;
-  fp.plan = sp.plan;
-  fp.slots_total = sp.slots_total;
-  const bool small = planned_merge_is_small(desc->batch, sp.Hkv * pl.R, fp.D);
-  const int rows_per_wg = (pl.balanced && !small ? 1024 : 256) / fp.D;   // merge workgroups: 256 threads, D per row, or D / 4
-  fp.nA = (sp.Hkv * pl.R + rows_per_wg - 1) / rows_per_wg;
-  const int nrows = (desc->collect_rows == VEGAS_COLLECT_ALL_ROWS) ? desc->num_queries
-                                                                   : (desc->num_queries > 1 ? 2 : 1);
-  fp.inv_norm = 1.0f / (static_cast<float>(nrows) * static_cast<float>(desc->num_q_heads));
-  // Every score workgroup (32 pages) rebuilds the row log-sum-exps from the (rows x chunks) table of
-  // (max, sum) pairs; giving a workgroup more pages to amortise that was measured slower.
-  const size_t hr = static_cast<size_t>(sp.Hkv) * pl.R;
-  int nB = (desc->max_blocks + 31) / 32;
-  // An upper bound of what the roles lay out (at most 13 x rows + 262 floats of collected rows, up to hr; verify_finalize_kernel), by which a
-  // call of more than 2394 rows is refused.
-  size_t shm = (hr + 256 + 16 * hr) * sizeof(float);
-  fp.nC = 0;
-  fp.tok_norm = 0.f;
-  if (logits) {                                        // token sums instead of page scores: 1024 tokens per workgroup
-    fp.nC = static_cast<int>((static_cast<int64_t>(desc->max_blocks) * kPage + 1023) / 1024);
-    fp.tok_norm = desc->softmax_scale / (static_cast<float>(nrows) * static_cast<float>(desc->num_q_heads));
-    nB = fp.nC;
-    shm = 272 * sizeof(float);
-  }
-  if (shm > 160 * 1024) return VEGAS_ERR_UNSUPPORTED;
-  const dim3 fgrid(fp.nA + nB, desc->batch);
-  auto launch_finalize = [&](auto kern) -> int {
-    if (int lrc = ensure_dynamic_lds(reinterpret_cast<const void*>(kern), shm)) return lrc;
-    hipLaunchKernelGGL(kern, fgrid, dim3(256), shm, st, fp);
-    return VEGAS_OK;
-  };
-  if (logits) {
-    if (pl.balanced && small) rc = launch_finalize(verify_finalize_kernel<kFinPlannedSmall, 1>);
-    else if (pl.balanced) rc = launch_finalize(verify_finalize_kernel<kFinPlanned, 1>);
-    else if (pl.nsplit <= 16) rc = launch_finalize(verify_finalize_kernel<16, 1>);
-    else if (pl.nsplit <= 32) rc = launch_finalize(verify_finalize_kernel<32, 1>);
-    else if (pl.nsplit <= 64) rc = launch_finalize(verify_finalize_kernel<64, 1>);
-    else rc = launch_finalize(verify_finalize_kernel<0, 1>);
-  } else {
-    if (pl.balanced && small) rc = launch_finalize(verify_finalize_kernel<kFinPlannedSmall>);
-    else if (pl.balanced) rc = launch_finalize(verify_finalize_kernel<kFinPlanned>);
-    else if (finalize_is_wide(sp.Hkv * pl.Rc, desc->batch, pl.nsplit)) {
-      if (pl.nsplit <= 16) rc = launch_finalize(verify_finalize_kernel<16, 0, kFinWideRounds>);
-      else rc = launch_finalize(verify_finalize_kernel<32, 0, kFinWideRounds>);
-    } else if (pl.nsplit <= 16) rc = launch_finalize(verify_finalize_kernel<16>);
-    else if (pl.nsplit <= 32) rc = launch_finalize(verify_finalize_kernel<32>);
-    else if (pl.nsplit <= 64) rc = launch_finalize(verify_finalize_kernel<64>);
-    else rc = launch_finalize(verify_finalize_kernel<0>);
-  }
-  if (rc != VEGAS_OK) return rc;
-  if (hipGetLastError() != hipSuccess) return VEGAS_ERR_LAUNCH;
-  return VEGAS_OK;
+  return launch_finalize(desc, pl, sp, logits, seq_lens, out, block_scores, st);
 }
 
 int vegas_select_blocks(const vegas_desc* desc, const float* block_scores, const int32_t* block_table,
@@ -1033,6 +1234,262 @@ int vegas_debug_draft_attention_stages(const vegas_desc* desc, const void* q, co
                                        void* workspace, size_t workspace_bytes, void* hip_stream, int32_t stages) {
   return draft_impl(desc, q, k_cache, v_cache, sel_table, sel_seq_lens, out, workspace, workspace_bytes, hip_stream,
                     stages);
+}
+
+size_t vegas_quant_workspace_bytes(const vegas_desc* desc) {
+  if (check_common(desc) != VEGAS_OK) return 0;
+  size_t need = kAlign;
+  QuantPlan pv, pd;
+  const int g = desc->num_q_heads / desc->num_kv_heads;
+  if (desc->num_queries > 0 && desc->num_queries <= 128 && check_paged16(desc) == VEGAS_OK &&
+      plan_quant(desc, desc->num_queries * g, desc->collect_rows != VEGAS_COLLECT_NONE, false, &pv) == VEGAS_OK)
+    need = pv.total > need ? pv.total : need;
+  if (plan_quant(desc, g, false, true, &pd) == VEGAS_OK) need = pd.total > need ? pd.total : need;
+  return need;
+}
+
+int vegas_verify_attention_quant(const vegas_desc* desc, const vegas_quant* cache, const void* q, const int32_t* block_table,
+                                 const int32_t* seq_lens, void* out, float* block_scores, void* workspace, size_t workspace_bytes,
+                                 void* hip_stream) {
+  int rc = check_common(desc);
+  if (rc == VEGAS_OK) rc = check_paged16(desc);
+  if (rc == VEGAS_OK) rc = check_quant(desc, cache);
+  if (rc != VEGAS_OK) return rc;
+  if (!q || !block_table || !seq_lens || !out) return VEGAS_ERR_NULL;
+  if (desc->num_queries <= 0 || desc->num_queries > 128) return desc->num_queries <= 0 ? VEGAS_ERR_SHAPE : VEGAS_ERR_UNSUPPORTED;
+  if (desc->collect_rows < 0 || desc->collect_rows > 2 || desc->window < 0) return VEGAS_ERR_SHAPE;
+  if (desc->score_metric != VEGAS_METRIC_PAGE_WEIGHTS && desc->score_metric != VEGAS_METRIC_TOKEN_LOGITS) return VEGAS_ERR_SHAPE;
+  const bool collect = desc->collect_rows != VEGAS_COLLECT_NONE;
+  if (desc->window != 0 || (collect && desc->score_metric != VEGAS_METRIC_PAGE_WEIGHTS)) return VEGAS_ERR_UNSUPPORTED;
+  QuantPlan pl;
+  rc = plan_quant(desc, desc->num_queries * (desc->num_q_heads / desc->num_kv_heads), collect, false, &pl);
+  if (rc != VEGAS_OK) return rc;
+  if (collect && !block_scores) return VEGAS_ERR_NULL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(block_table) || (block_scores && !aligned16(block_scores))) return VEGAS_ERR_ALIGN;
+  if (!workspace || workspace_bytes < pl.total) return VEGAS_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign) return VEGAS_ERR_ALIGN;
+  if (exceeds_quant_grid(desc, pl)) return VEGAS_ERR_UNSUPPORTED;
+  if (collect && finalize_lds(desc, pl) > 160 * 1024) return VEGAS_ERR_UNSUPPORTED;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  SplitParams sp;
+  fill_split_params(desc, pl, desc->num_queries, q, cache->k, cache->v, block_table, desc->max_blocks, seq_lens,
+                    static_cast<unsigned char*>(workspace), &sp);
+  sp.row_blocks = pl.NB | quant_groups(pl) << 8;
+  if (pl.balanced) sp.share_group = 8;                             // (eight consecutive chunks start on as many XCDs)
+  rc = launch_quant(desc, cache, pl, sp, false, collect, st);
+  if (rc != VEGAS_OK) return rc;
+  return collect ? launch_finalize(desc, pl, sp, false, seq_lens, out, block_scores, st) : launch_combine(desc, pl, sp, out, st);
+}
+
+int vegas_draft_attention_quant(const vegas_desc* desc, const vegas_quant* cache, const void* q, const int32_t* sel_table,
+                                const int32_t* sel_seq_lens, void* out, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_common(desc);
+  if (rc == VEGAS_OK) rc = check_quant(desc, cache);
+  if (rc != VEGAS_OK) return rc;
+  if (!q || !sel_table || !sel_seq_lens || !out) return VEGAS_ERR_NULL;
+  if (desc->max_sel_blocks <= 0) return VEGAS_ERR_SHAPE;
+  if (static_cast<int64_t>(desc->max_seq_len) > static_cast<int64_t>(desc->max_sel_blocks) * desc->page_size) return VEGAS_ERR_SHAPE;
+  QuantPlan pl;
+  rc = plan_quant(desc, desc->num_q_heads / desc->num_kv_heads, false, true, &pl);
+  if (rc != VEGAS_OK) return rc;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(sel_table)) return VEGAS_ERR_ALIGN;
+  if (!workspace || workspace_bytes < pl.total) return VEGAS_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign) return VEGAS_ERR_ALIGN;
+  if (exceeds_quant_grid(desc, pl)) return VEGAS_ERR_UNSUPPORTED;
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  SplitParams sp;
+  fill_split_params(desc, pl, 1, q, cache->k, cache->v, sel_table, desc->max_sel_blocks, sel_seq_lens, static_cast<unsigned char*>(workspace), &sp);
+  sp.row_blocks = pl.NB | quant_groups(pl) << 8;
+  const bool direct = pl.nsplit == 1;
+  if (direct) sp.out_direct = static_cast<uint16_t*>(out);
+  rc = launch_quant(desc, cache, pl, sp, true, false, st);
+  if (rc != VEGAS_OK || direct) return rc;
+  return launch_combine(desc, pl, sp, out, st);
+}
+
+int vegas_rope_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, int64_t original_len, double beta_fast,
+                           double beta_slow, double* inv_freq, float* magnitude) {
+  if (!inv_freq || !magnitude) return VEGAS_ERR_NULL;
+  if (rot_dim <= 0 || rot_dim % 2 || !(base > 1.0) || !std::isfinite(base)) return VEGAS_ERR_SHAPE;
+  if (scaling < VEGAS_ROPE_SCALE_NONE || scaling > VEGAS_ROPE_SCALE_YARN) return VEGAS_ERR_UNSUPPORTED;
+  if (scaling != VEGAS_ROPE_SCALE_NONE && (!(factor >= 1.0) || !std::isfinite(factor))) return VEGAS_ERR_SHAPE;
+  const bool yarn = scaling == VEGAS_ROPE_SCALE_YARN;
+  if (yarn && (original_len <= 0 || !(beta_slow > 0.0) || !(beta_fast > beta_slow) || !std::isfinite(beta_fast))) return VEGAS_ERR_SHAPE;
+  constexpr double kTurn = 6.283185307179586476925;
+  if (scaling == VEGAS_ROPE_SCALE_NTK && rot_dim > 2) base *= std::pow(factor, rot_dim / (rot_dim - 2.0));
+  // YaRN (Peng et al. 2023, Sec. 3.2): dims that turn more than beta_fast times over the original length keep their frequency, those below
+  // beta_slow turns are interpolated, a ramp over the pair index between.
+  auto pair_of = [&](double turns) { return rot_dim * std::log(static_cast<double>(original_len) / (turns * kTurn)) / (2.0 * std::log(base)); };
+  double low = 0.0, span = 1.0;
+  if (yarn) {
+    low = std::fmax(std::floor(pair_of(beta_fast)), 0.0);
+    const double high = std::fmin(std::ceil(pair_of(beta_slow)), rot_dim - 1.0);
+    span = std::fmax(high - low, 0.001);
+  }
+  for (int32_t i = 0; i < rot_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rot_dim);
+    if (scaling == VEGAS_ROPE_SCALE_LINEAR) f /= factor;
+    if (yarn) {
+      const double ramp = std::fmin(std::fmax((i - low) / span, 0.0), 1.0);
+      f = f / factor * ramp + f * (1.0 - ramp);
+    }
+    inv_freq[i] = f;
+  }
+  *magnitude = yarn ? static_cast<float>(0.1 * std::log(factor) + 1.0) : 1.0f;
+  return VEGAS_OK;
+}
+
+int vegas_rotate(const vegas_rope* rope, int32_t head_dim, int64_t num_tokens, int32_t num_heads, const int32_t* positions, const void* x,
+                 int64_t x_token_stride, int64_t x_head_stride, void* out, int64_t out_token_stride, int64_t out_head_stride,
+                 void* hip_stream) {
+  if (head_dim != 128 && head_dim != 64) return VEGAS_ERR_UNSUPPORTED;
+  if (int rc = check_rope(rope, head_dim)) return rc;
+  if (num_tokens < 0 || num_heads <= 0) return VEGAS_ERR_SHAPE;
+  if (num_tokens > INT32_MAX || num_heads > 65535) return VEGAS_ERR_UNSUPPORTED;
+  if (!positions || !x || !out) return VEGAS_ERR_NULL;
+  if (x_head_stride < head_dim || x_token_stride < head_dim || out_head_stride < head_dim || out_token_stride < head_dim) return VEGAS_ERR_SHAPE;
+  if (x == out && (x_token_stride != out_token_stride || x_head_stride != out_head_stride)) return VEGAS_ERR_SHAPE;
+  if (!aligned16(x) || !aligned16(out) || ((x_token_stride | x_head_stride | out_token_stride | out_head_stride) % 8)) return VEGAS_ERR_ALIGN;
+  if (num_tokens == 0) return VEGAS_OK;
+  RotateParams p;
+  p.rope = rope_params(rope);
+  p.positions = positions;
+  p.x = static_cast<const uint16_t*>(x);
+  p.out = static_cast<uint16_t*>(out);
+  p.x_token = x_token_stride; p.x_head = x_head_stride; p.out_token = out_token_stride; p.out_head = out_head_stride;
+  p.N = static_cast<int32_t>(num_tokens);
+  p.H = num_heads;
+  const int rows = 64 / (head_dim / kUnit), all = (num_heads + rows - 1) / rows;
+  p.steps = wave_steps(num_tokens, all);
+  const dim3 grid(static_cast<unsigned>((num_tokens + 3) / 4), (all + p.steps - 1) / p.steps);
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (head_dim == 128) hipLaunchKernelGGL(rotate_kernel<128>, grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL(rotate_kernel<64>, grid, dim3(256), 0, st, p);
+  return hipGetLastError() == hipSuccess ? VEGAS_OK : VEGAS_ERR_LAUNCH;
+}
+
+int vegas_append_quant(const vegas_desc* desc, const vegas_quant* cache, const vegas_rope* rope, const vegas_new_tokens* tokens,
+                       const int32_t* block_table, const int32_t* seq_lens, int32_t* seq_lens_out, int32_t* sel_table,
+                       int32_t* sel_seq_lens, int32_t sel_page_size, void* hip_stream) {
+  int rc = check_common(desc);
+  if (rc == VEGAS_OK) rc = check_paged16(desc);
+  if (rc == VEGAS_OK) rc = check_quant(desc, cache);
+  if (rc == VEGAS_OK && rope) rc = check_rope(rope, desc->head_dim);
+  if (rc != VEGAS_OK) return rc;
+  if (!tokens || !tokens->k || !tokens->v || !block_table || !seq_lens || !seq_lens_out) return VEGAS_ERR_NULL;
+  if ((tokens->q == nullptr) != (tokens->q_out == nullptr)) return VEGAS_ERR_NULL;
+  if (tokens->q && !rope) return VEGAS_ERR_NULL;
+  if (tokens->num_new <= 0 || tokens->reserved != 0) return VEGAS_ERR_SHAPE;
+  if (tokens->num_new > (1 << 24)) return VEGAS_ERR_UNSUPPORTED;
+  if ((sel_table == nullptr) != (sel_seq_lens == nullptr)) return VEGAS_ERR_NULL;
+  if (sel_table && desc->max_sel_blocks <= 0) return VEGAS_ERR_SHAPE;
+  if (sel_table && sel_page_size != kPage && sel_page_size != 1) return VEGAS_ERR_UNSUPPORTED;
+  const int64_t kv_row = static_cast<int64_t>(desc->num_kv_heads) * desc->head_dim, q_row = static_cast<int64_t>(desc->num_q_heads) * desc->head_dim;
+  const int64_t kv_token = tokens->kv_token_stride ? tokens->kv_token_stride : kv_row;
+  const int64_t q_token = tokens->q_token_stride ? tokens->q_token_stride : q_row;
+  const int64_t q_out_token = tokens->q_out_token_stride ? tokens->q_out_token_stride : q_row;
+  if (kv_token < kv_row || q_token < q_row || q_out_token < q_row) return VEGAS_ERR_SHAPE;
+  if (tokens->q && tokens->q == tokens->q_out && q_token != q_out_token) return VEGAS_ERR_SHAPE;
+  if (!aligned16(tokens->k) || !aligned16(tokens->v) || !aligned16(tokens->q) || !aligned16(tokens->q_out) || ((kv_token | q_token | q_out_token) % 8))
+    return VEGAS_ERR_ALIGN;
+  QuantAppendParams p;
+  p.rope = rope_params(rope);
+  p.k_new = static_cast<const uint16_t*>(tokens->k);
+  p.v_new = static_cast<const uint16_t*>(tokens->v);
+  p.q = static_cast<const uint16_t*>(tokens->q);
+  p.q_out = static_cast<uint16_t*>(tokens->q_out);
+  p.new_lens = tokens->new_lens;
+  p.kv_token = kv_token; p.q_token = q_token; p.q_out_token = q_out_token;
+  p.k_cache = static_cast<uint8_t*>(cache->k);
+  p.v_cache = static_cast<uint8_t*>(cache->v);
+  p.scales = cache->scales;
+  p.block_table = block_table;
+  p.seq_lens = seq_lens;
+  p.T = tokens->num_new;
+  p.Hkv = desc->num_kv_heads;
+  p.Hq = desc->num_q_heads;
+  p.max_blocks = desc->max_blocks;
+  p.max_tokens = desc->max_seq_len;
+  p.page_stride = desc->kv_page_stride;
+  p.token_stride = desc->kv_token_stride;
+  p.head_stride = desc->kv_head_stride;
+  p.num_pages = desc->num_pages;
+  p.grow.block_table = block_table;
+  p.grow.seq_lens = nullptr;
+  p.grow.sel_table = sel_table;
+  p.grow.sel_seq_lens = sel_seq_lens;
+  p.grow.batch = desc->batch;
+  p.grow.num_new = 0;
+  p.grow.max_blocks = desc->max_blocks;
+  p.grow.max_sel_blocks = desc->max_sel_blocks;
+  p.grow.page_size = sel_page_size;
+  const int rows = 64 / (desc->head_dim / kUnit);
+  const int all = 2 * ((p.Hkv + rows - 1) / rows) + (p.q ? (p.Hq + rows - 1) / rows : 0);
+  // Lengths stored where they were read: a few tokens are one workgroup's work, which stores them last; more take a second launch.
+  const bool in_place = seq_lens == seq_lens_out;
+  const bool one_workgroup = in_place && static_cast<int64_t>(p.T) * all <= kOneWorkgroupSteps;
+  p.seq_lens_out = in_place && !one_workgroup ? nullptr : seq_lens_out;
+  p.steps = wave_steps(static_cast<int64_t>(desc->batch) * p.T, all);
+  p.tokens = p.T >= 64 ? kPage : 4;          // (a page's scales are written by one workgroup, or two)
+  const dim3 grid = one_workgroup ? dim3(1, 1, desc->batch) : dim3((p.T + p.tokens - 1) / p.tokens, (all + p.steps - 1) / p.steps, desc->batch);
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  auto launch = [&](auto dim, auto format) {
+    constexpr int D = decltype(dim)::value, FMT = decltype(format)::value;
+    if (one_workgroup) hipLaunchKernelGGL((append_quant_kernel<D, FMT, true>), grid, dim3(1024), 0, st, p);
+    else hipLaunchKernelGGL((append_quant_kernel<D, FMT, false>), grid, dim3(256), 0, st, p);
+  };
+  auto by_format = [&](auto dim) {
+    if (cache->format == VEGAS_QUANT_E4M3) launch(dim, std::integral_constant<int, kE4m3>{});
+    else launch(dim, std::integral_constant<int, kInt8>{});
+  };
+  if (desc->head_dim == 128) by_format(std::integral_constant<int, 128>{});
+  else by_format(std::integral_constant<int, 64>{});
+  if (hipGetLastError() != hipSuccess) return VEGAS_ERR_LAUNCH;
+  if (p.seq_lens_out == nullptr) {
+    hipLaunchKernelGGL(advance_lengths_kernel, dim3((desc->batch + 63) / 64), dim3(64), 0, st, p, seq_lens_out, desc->batch);
+    if (hipGetLastError() != hipSuccess) return VEGAS_ERR_LAUNCH;
+  }
+  return VEGAS_OK;
+}
+
+int vegas_read_quant(const vegas_desc* desc, const vegas_quant* cache, const int32_t* table, const int32_t* lens, const int32_t* first,
+                     int32_t num_tokens, void* k_out, void* v_out, void* hip_stream) {
+  int rc = check_common(desc);
+  if (rc == VEGAS_OK) rc = check_quant(desc, cache);
+  if (rc != VEGAS_OK) return rc;
+  if (!table || !lens || !k_out || !v_out) return VEGAS_ERR_NULL;
+  if (desc->max_sel_blocks <= 0 || num_tokens <= 0) return VEGAS_ERR_SHAPE;
+  if (static_cast<int64_t>(desc->max_seq_len) > static_cast<int64_t>(desc->max_sel_blocks) * desc->page_size) return VEGAS_ERR_SHAPE;
+  if (num_tokens > (1 << 30)) return VEGAS_ERR_UNSUPPORTED;
+  if (!aligned16(k_out) || !aligned16(v_out)) return VEGAS_ERR_ALIGN;
+  QuantReadParams p;
+  p.k_cache = static_cast<const uint8_t*>(cache->k);
+  p.v_cache = static_cast<const uint8_t*>(cache->v);
+  p.scales = cache->scales;
+  p.table = table;
+  p.lens = lens;
+  p.first = first;
+  p.k_out = static_cast<uint16_t*>(k_out);
+  p.v_out = static_cast<uint16_t*>(v_out);
+  p.T = num_tokens;
+  p.Hkv = desc->num_kv_heads;
+  p.table_stride = desc->max_sel_blocks;
+  p.max_tokens = desc->max_seq_len;
+  p.page_shift = page_shift_of(desc->page_size);
+  p.page_stride = desc->kv_page_stride;
+  p.token_stride = desc->kv_token_stride;
+  p.head_stride = desc->kv_head_stride;
+  p.num_pages = desc->num_pages;
+  const dim3 grid((num_tokens + kReadTokens - 1) / kReadTokens, 1, desc->batch);
+  hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  auto launch = [&](auto dim) {
+    constexpr int D = decltype(dim)::value;
+    if (cache->format == VEGAS_QUANT_E4M3) hipLaunchKernelGGL((read_quant_kernel<D, kE4m3>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((read_quant_kernel<D, kInt8>), grid, dim3(256), 0, st, p);
+  };
+  if (desc->head_dim == 128) launch(std::integral_constant<int, 128>{});
+  else launch(std::integral_constant<int, 64>{});
+  return hipGetLastError() == hipSuccess ? VEGAS_OK : VEGAS_ERR_LAUNCH;
 }
 
 int vegas_debug_stream_read(const void* a, const void* b, size_t bytes_each, int32_t workgroups, int32_t non_temporal,
