@@ -428,9 +428,8 @@ size_t vegas_quant_workspace_bytes(const vegas_desc* desc);
 
 /*
  * vegas_verify_attention over an 8-bit cache: the same arguments and outputs, with the values that the codes stand for as K
- * and V; `workspace` is of at least vegas_quant_workspace_bytes(desc) bytes.  VEGAS_ERR_UNSUPPORTED for a local mask (desc->window) and for score_metric VEGAS_METRIC_TOKEN_LOGITS when
- * collecting; a caller's kv_chunk_tokens is refused where the page scores of one chunk do not fit a workgroup (with 128 rows
- * from 10000 tokens on).
+ * and V; `workspace` is of at least vegas_quant_workspace_bytes(desc) bytes.  VEGAS_ERR_UNSUPPORTED for a local mask
+ * (desc->window), and for score_metric VEGAS_METRIC_TOKEN_LOGITS when collecting.
  */
 int vegas_verify_attention_quant(const vegas_desc* desc, const vegas_quant* cache, const void* q, const int32_t* block_table,
                                  const int32_t* seq_lens, void* out, float* block_scores, void* workspace,

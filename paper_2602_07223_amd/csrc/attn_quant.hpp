@@ -15,11 +15,14 @@
 //   * Scales: a wave's 32 + 32 of a tile are one dword per lane, spread through LDS (four 16-byte reads) instead of being
 //     loaded by all 16 lanes that use them.
 //   * NT tiles of 16 query rows share a tile's loads and conversions.
-//   * A row's reference m follows its maximum only when that has grown by more than 2^6: weights are then below 2^6 and the
+//   * A row's base follows its maximum only when that has grown by more than 2^6: weights are then below 2^6 and the
 //     usual rescaling of the outputs, and the reduction over the four lanes of a row, is seldom met.
-// What bounds it: memory from 64 MB on.  A 32-token tile of a head is 8.25 KB (D = 128), half of the bf16 cache's, and costs 80
-// conversions (e4m3; int8 192) and per 16 rows 16 MFMAs and about 90 vector instructions.  Loads run a whole tile ahead in a second set of
-// registers.
+// What bounds it: memory from 64 MB on, latencies below.  A 32-token tile of a head is 8.25 KB (D = 128), half of the bf16 cache's, and costs 80
+// conversions (e4m3; int8 192) and per 16 rows 16 MFMAs and about 90 vector instructions; a copy that only loads its tiles takes 270 us
+// where the kernel with 40 rows takes 285.  Loads run a whole tile ahead in a second set of registers; three to five tiles ahead
+// were no faster.  Captured calls with their merges: verification of 16 sequences of 8192..65536 tokens, 40 rows, 8 KV heads (1.26 GB)
+// 284 us, without scores 226 (5.5 TB/s; the log-sum-exps, 47 MB written and read again, make the difference), 20 rows and 36864 tokens
+// each 218 (5.7 TB/s); one sequence of 32768, 20 rows 26.4; draft calls, 12 of 1000..48000 (642 MB) 111 (5.8 TB/s), one of 2080 6.9.
 // TOKENS: the page list has pages of fewer than 16 tokens (page_shift): every lane works out the address of one token
 // of the tile, the wave shares them through LDS.
 #pragma once
@@ -35,20 +38,23 @@ struct QuantArgs {
   const float* scales;       // [page, KV head, 2, 16]
   int32_t page_shift;        // log2 of the page list's tokens per page
   int32_t park_bytes;        // dynamic LDS of the page log-sum-exps (COLLECT) or of the merge, whichever is larger
+  int32_t park_tiles;        // COLLECT: tiles whose log-sum-exps a wave holds back (even)
 };
 
-constexpr int kQuantVerifyNT = 3, kQuantDraftNT = 2;   // 16-row tiles of a workgroup, at most (what registers hold)
+constexpr int kQuantCollectNT = 3, kQuantNT = 2;       // 16-row tiles of a workgroup that collects, and of others, at most: what registers hold
+constexpr int kQuantVerifyWaves = 8, kQuantDraftWaves = 4;      // waves of a workgroup (wide ones, of long calls, and narrow ones)
+constexpr int kQuantHeads = 4;                // KV heads of a workgroup, at most
 constexpr float kQuantSlack = 6.f;           // log2 of how far weights may pass 1
 
-// Dynamic LDS: [parked page log-sum-exps | merge rows, NW x 16] [queries, 16 NT rows] [row maxima, sums][scales, addresses of a wave]
+// Dynamic LDS: [parked page log-sum-exps | merge rows, NW x 16] [queries, 16 NT rows a head] [row maxima, sums][scales, addresses of a wave]
 constexpr size_t quant_merge_bytes(int NW, int D) { return static_cast<size_t>(NW) * 16 * red_pitch(D) * sizeof(float); }
-constexpr size_t quant_tail_bytes(int NW, int NT, int D) {
-  return (NT > 1 ? static_cast<size_t>(16) * NT * row_pitch(D) : 0) + 2 * static_cast<size_t>(NW) * 16 * NT * sizeof(float) +
+constexpr size_t quant_tail_bytes(int NW, int NT, int D, int heads) {
+  return (NT > 1 ? static_cast<size_t>(heads) * 16 * NT * row_pitch(D) : 0) + 2 * static_cast<size_t>(NW) * 16 * NT * sizeof(float) +
          static_cast<size_t>(NW) * (64 * sizeof(float) + 32 * sizeof(uint64_t));
 }
-inline size_t quant_park_bytes(int NW, int rows, int chunk_tokens, bool collect, int D) {
-  const size_t merge = quant_merge_bytes(NW, D);
-  const size_t park = collect ? (static_cast<size_t>(chunk_tokens) / kPage * rows * sizeof(float) + 15) / 16 * 16 : 0;
+// (A wave writes its log-sum-exps when park_tiles tiles have some, and up to two more may follow before it looks.)
+constexpr size_t quant_park_bytes(int NW, int rows, int park_tiles, bool collect, int D) {
+  const size_t merge = quant_merge_bytes(NW, D), park = collect ? static_cast<size_t>(NW) * (park_tiles + 2) * 2 * rows * sizeof(float) : 0;
   return park > merge ? park : merge;
 }
 
@@ -107,54 +113,63 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, kg = lane >> 4;
-  // Grid (chunk in a group of 8, KV head + Hkv * row block, group + groups * sequence).  Workgroups go round the 8 XCDs, so a chunk's heads and
-  // row blocks meet on one of them, which then reads whole pages: 16 x 128 bytes of a token at a time.  (Heads first, an XCD reads every eighth
-  // 128-byte line: @@)
-  const int row_blocks = p.row_blocks & 255, groups = p.row_blocks >> 8;
-  int h = blockIdx.y, rb = 0;
+  // Grid (chunk in a group of `across` <= 8, heads of a workgroup + Hkv / HP * row block, group + groups * sequence).  HP neighbouring KV heads share a
+  // workgroup, wave w has head w % HP of them: their rows of a token are consecutive 128-byte lines, asked for at about the same time.
+  // (A plain read of the lines alone, 16-token pages in random order, 1.2 GB: heads each by itself 5.7 TB/s, two together 6.4, four 6.8,
+  // eight 6.9, head-major pages 6.9.)  Workgroups go round the 8 XCDs, so a chunk's heads and row blocks meet on one of them.
+  constexpr bool WIDE = NW == kQuantVerifyWaves;       // (only such workgroups have several heads, or a plan)
+  const int row_blocks = p.row_blocks & 15, hp_shift = WIDE ? (p.row_blocks >> 4) & 15 : 0;
+  const int across = (p.row_blocks >> 8) & 15, groups = p.row_blocks >> 12;
+  const int HP = 1 << hp_shift, sub = wave & (HP - 1), wv = wave >> hp_shift, NWH = NW >> hp_shift;   // NWH: waves of a head
+  int hg = blockIdx.y, rb = 0;
   if (row_blocks > 1) {
-    rb = static_cast<int>(blockIdx.y) / p.Hkv;
-    h -= rb * p.Hkv;
+    const int per_block = p.Hkv >> hp_shift;
+    rb = static_cast<int>(blockIdx.y) / per_block;
+    hg -= rb * per_block;
   }
-  int b = blockIdx.z, split = blockIdx.x;
-  if (groups > 1) {                          // (z < 2^16: the quotient is exact)
-    b = static_cast<int>((static_cast<float>(blockIdx.z) + 0.5f) * __builtin_amdgcn_rcpf(static_cast<float>(groups)));
-    split += 8 * (static_cast<int>(blockIdx.z) - b * groups);
+  const int h0 = hg << hp_shift, h = h0 + sub;
+  // (z < 2^16: the quotients are exact.  Chunks are turned by one from sequence to sequence: a ragged batch's last ones, which are short or
+  // empty, would all be the same XCDs'.  96 sequences of 500..20000 tokens, 8 KV heads, chunks of 2048: 550 -> 402 us.)
+  auto over = [](int a, int d) { return static_cast<int>((static_cast<float>(a) + 0.5f) * __builtin_amdgcn_rcpf(static_cast<float>(d))); };
+  int b = blockIdx.z, group = 0;
+  if (groups > 1) {
+    b = over(blockIdx.z, groups);
+    group = static_cast<int>(blockIdx.z) - b * groups;
   }
+  int split = static_cast<int>(blockIdx.x) + b + group;
+  split += 8 * group - across * over(split, across);
   int chunk_tokens = p.chunk_tokens;
   int c0 = split * chunk_tokens;
   int slot = split;
   int n = 0;
-  if constexpr (!TOKENS) {
-    if (p.plan) {                            // (groups is 1: no sequence in the grid) balanced chunking: workgroup `split` of this head -> (sequence, tokens)
-      split = static_cast<int>(blockIdx.x + 8 * blockIdx.z);
-      const BalancedSlot bs = balanced_slot(p.lens, p.batch, p.max_tokens, p.slots_target, p.slots_target2, p.share_group,
-                                            p.slots_total, p.share_margin, 2, p.chunk_cap_units, kTile * NW, split,
-                                            ((blockIdx.x | blockIdx.y | blockIdx.z) == 0 && wave == 0) ? p.plan : nullptr);
-      b = __builtin_amdgcn_readfirstlane(bs.b);
-      if (b < 0) return;
-      c0 = __builtin_amdgcn_readfirstlane(bs.c0);
-      chunk_tokens = __builtin_amdgcn_readfirstlane(bs.chunk);
-      slot = __builtin_amdgcn_readfirstlane(bs.slot);
-      n = bs.n;
-    }
+  if (WIDE && p.plan) {                      // (groups is 1: no sequence in the grid) balanced chunking: workgroup `split` of this head -> (sequence, tokens)
+    split = static_cast<int>(blockIdx.x + 8 * blockIdx.z);
+    const BalancedSlot bs = balanced_slot(p.lens, p.batch, p.max_tokens, p.slots_target, p.slots_target2, p.share_group,
+                                          p.slots_total, p.share_margin, 2, p.chunk_cap_units, kTile * NWH, split,
+                                          ((blockIdx.x | blockIdx.y | blockIdx.z) == 0 && wave == 0) ? p.plan : nullptr);
+    b = __builtin_amdgcn_readfirstlane(bs.b);
+    if (b < 0) return;
+    c0 = __builtin_amdgcn_readfirstlane(bs.c0);
+    chunk_tokens = __builtin_amdgcn_readfirstlane(bs.chunk);
+    slot = __builtin_amdgcn_readfirstlane(bs.slot);
+    n = bs.n;
   }
   const int row0 = rb * 16 * NT;             // first row (of this KV head) handled here
   const int Rl = min(16 * NT, p.R - row0);
 
   // ---- one round trip for what the preloaded arguments can address: page ids, length, queries (see attn_split_kernel)
   const int32_t* table = p.table + static_cast<int64_t>(b) * p.table_stride;
-  const int tile_first = c0 / kTile + wave;
+  const int tile_first = c0 / kTile + wv;
   int last_page = 0;                         // (set below)
-  // 16-token pages: ids of the wave's next 32 tiles, lane (k, half) <-> page `half` of tile tile_first + k NW.
+  // 16-token pages: ids of the wave's next 32 tiles, lane (k, half) <-> page `half` of tile tile_first + k NWH.
   auto table_entry = [&](int kbase) -> int {
-    int page = 2 * (tile_first + (kbase + (lane & 31)) * NW) + (lane >> 5);
+    int page = 2 * (tile_first + (kbase + (lane & 31)) * NWH) + (lane >> 5);
     page = page < p.table_stride ? page : p.table_stride - 1;
     return table[page];
   };
   // Page lists: id of the page of token lane % 32 of tile k.
   auto ids_entry = [&](int k) -> int {
-    const int64_t tok = static_cast<int64_t>(tile_first + k * NW) * kTile + (lane & 31);
+    const int64_t tok = static_cast<int64_t>(tile_first + k * NWH) * kTile + (lane & 31);
     const int64_t page = tok >> qa.page_shift;
     return table[page < p.table_stride ? page : p.table_stride - 1];
   };
@@ -162,29 +177,36 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
   int first_entry = TOKENS ? ids_entry(0) : table_entry(0);
   int zero = 0;
   asm("" : "+v"(zero));                      // (a vector load: a scalar one is waited for at once)
-  if (!p.plan) n = p.lens[b + zero];
+  if (!WIDE || !p.plan) n = p.lens[b + zero];
 
   // Queries: lane (row l16, kg) of tile nt, step 2 j + u: dims 64 j + 16 kg + 8 u .. + 7.  One tile's stay in registers, more go through LDS.
   const float rcp_g = __builtin_amdgcn_rcpf(static_cast<float>(p.g));
-  const unsigned char* qbase = uniform_ptr(reinterpret_cast<const unsigned char*>(p.q + (static_cast<int64_t>(b) * p.G * p.Hq + h * p.g) * D));
+  const unsigned char* qbase = uniform_ptr(reinterpret_cast<const unsigned char*>(p.q + (static_cast<int64_t>(b) * p.G * p.Hq + (NT == 1 ? h : h0) * p.g) * D));
   auto row_token = [&](int r) { return static_cast<int>((static_cast<float>(r) + 0.5f) * rcp_g); };   // (r < 128: exact)
   constexpr bool QREG = NT == 1;
-  u32x4 qreg[QREG ? KS : 1];
+  u32x4 qreg[QREG ? NT : 1][KS];
   constexpr int QI = QREG ? 1 : (16 * NT * (D / 8) + NW * 64 - 1) / (NW * 64);
-  u32x4 qraw[QI];
+  constexpr int kHeads = QREG ? 1 : kQuantHeads;       // (of more tiles every head's rows are in LDS)
+  u32x4 qraw[kHeads][QI];
   int row_lim[NT];                           // token of the row, later the last position it sees
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) row_lim[nt] = row_token(row0 + min(16 * nt + l16, Rl - 1));
   if constexpr (QREG) {
-    const int r = row0 + min(l16, Rl - 1);
-    const uint32_t off = static_cast<uint32_t>(row_lim[0] * p.Hq + (r - row_lim[0] * p.g)) * (2u * D);
 #pragma unroll
-    for (int s = 0; s < KS; ++s) qreg[s] = gload<u32x4, false>(qbase, off + static_cast<uint32_t>(64 * (s >> 1) + 16 * kg + 8 * (s & 1)) * 2u);
+    for (int nt = 0; nt < NT; ++nt) {
+      const int r = row0 + min(16 * nt + l16, Rl - 1);
+      const uint32_t off = static_cast<uint32_t>(row_lim[nt] * p.Hq + (r - row_lim[nt] * p.g)) * (2u * D);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) qreg[nt][s] = gload<u32x4, false>(qbase, off + static_cast<uint32_t>(64 * (s >> 1) + 16 * kg + 8 * (s & 1)) * 2u);
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < QI; ++i) {
       const int idx = tid + i * NW * 64, r = row0 + min(idx / (D / 8), Rl - 1), t = row_token(r);
-      qraw[i] = gload<u32x4, false>(qbase, static_cast<uint32_t>((t * p.Hq + (r - t * p.g)) * D + (idx % (D / 8)) * 8) * 2u);
+      const uint32_t off = static_cast<uint32_t>((t * p.Hq + (r - t * p.g)) * D + (idx % (D / 8)) * 8) * 2u;
+#pragma unroll
+      for (int s = 0; s < kHeads; ++s)
+        if (s < HP) qraw[s][i] = gload<u32x4, false>(qbase, off + static_cast<uint32_t>(s * p.g) * (2u * D));
     }
   }
   asm volatile("" : "+s"(p.k), "+s"(p.v), "+s"(p.page_stride), "+s"(p.token_stride), "+s"(p.head_stride), "+s"(p.num_pages),
@@ -193,21 +215,25 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
   n = __builtin_amdgcn_readfirstlane(n);
   n = n < 0 ? 0 : (n > p.max_tokens ? p.max_tokens : n);
   last_page = static_cast<int>(p.num_pages < INT32_MAX ? p.num_pages - 1 : INT32_MAX);
-  const int64_t pbase = p.plan ? static_cast<int64_t>(h) * p.slots_total + slot : (static_cast<int64_t>(b) * p.Hkv + h) * p.nsplit + slot;
+  // partial slot of head h0 + s: pbase + s * slots
+  const bool planned = WIDE && p.plan;
+  const int64_t slots = planned ? p.slots_total : p.nsplit;
+  const int64_t pbase = (planned ? 0 : static_cast<int64_t>(b) * p.Hkv * p.nsplit) + h0 * slots + slot;
 
   unsigned char* qlds = smem + qa.park_bytes;
-  float* sm_m = reinterpret_cast<float*>(qlds + (NT > 1 ? 16 * NT * row_pitch(D) : 0));      // [wave][16 NT]
+  float* sm_m = reinterpret_cast<float*>(qlds + (NT > 1 ? HP * 16 * NT * row_pitch(D) : 0));      // [wave][16 NT]
+  const unsigned char* const my_q = qlds + sub * 16 * NT * row_pitch(D);
   float* sm_l = sm_m + NW * 16 * NT;
   float* scale_lds = sm_l + NW * 16 * NT + wave * 64;                                        // [K: 32][V: 32] of a tile
   uint64_t* addr_lds = reinterpret_cast<uint64_t*>(sm_l + NW * 16 * NT + NW * 64) + wave * 32;
-  float* lse_lds = reinterpret_cast<float*>(smem);                                           // [pages of the chunk][Rl]
+  float* lse_lds = reinterpret_cast<float*>(smem) + wave * (qa.park_tiles + 2) * 2 * Rl;     // [tile][page][Rl] of this wave
   float* red = reinterpret_cast<float*>(smem);
 
   if (__builtin_expect(c0 >= n, 0)) {        // nothing to do, no partial is read
     if (p.out_direct != nullptr) {           // no merge kernel follows: the rows of an empty sequence are zeros
-      for (int e = tid; e < Rl * D; e += NW * 64) {
-        const int r = row0 + e / D, t = r / p.g;
-        p.out_direct[((static_cast<int64_t>(b) * p.G + t) * p.Hq + h * p.g + (r - t * p.g)) * D + e % D] = 0;
+      for (int e = tid; e < HP * Rl * D; e += NW * 64) {
+        const int s = e / (Rl * D), r = row0 + (e - s * Rl * D) / D, t = r / p.g;
+        p.out_direct[((static_cast<int64_t>(b) * p.G + t) * p.Hq + (h0 + s) * p.g + (r - t * p.g)) * D + e % D] = 0;
       }
     }
     return;
@@ -215,7 +241,7 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
   VEGAS_TL(kTlLength);
   const int c1 = min(c0 + chunk_tokens, n);
   const int tile_end = (c1 + kTile - 1) / kTile;
-  const int ntiles = tile_first < tile_end ? (tile_end - tile_first + NW - 1) / NW : 0;
+  const int ntiles = tile_first < tile_end ? (tile_end - tile_first + NWH - 1) / NWH : 0;
   const int sees = n - p.G;                  // last position that row 0 sees
   const int64_t head_off = static_cast<int64_t>(h) * p.head_stride;
   const unsigned char* k_head = reinterpret_cast<const unsigned char*>(p.k) + head_off;
@@ -241,8 +267,10 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
     return (gbytes)(reinterpret_cast<const unsigned char*>(qa.scales)) + ((page16 * p.Hkv + h) * 32 + (lane >> 5) * 16 + in_page) * 4;
   };
   auto issue = [&](int k, Tile& t) {
+    uint32_t k_off = k_lane_off, v_off = v_lane_off;
+    asm volatile("" : "+v"(k_off), "+v"(v_off));                  // (32-bit offsets of scalar bases stay that)
     if constexpr (TOKENS) {
-      const int tok = lane & 31, in_page = ((tile_first + k * NW) * kTile + tok) & ((1 << qa.page_shift) - 1);
+      const int tok = lane & 31, in_page = ((tile_first + k * NWH) * kTile + tok) & ((1 << qa.page_shift) - 1);
       const int64_t id = into_pool(ids_next);
       ids_next = ids_entry(k + 1);
       const int64_t pool_slot = (id << qa.page_shift) + in_page;
@@ -266,10 +294,10 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
-        for (int j = 0; j < KL; ++j) t.k[pg][j] = gload<u32x4, NT_LOADS>(uniform_ptr(k_head + (pg ? at1 : at0)) + static_cast<uint32_t>(8 * j) * ts, k_lane_off);
+        for (int j = 0; j < KL; ++j) t.k[pg][j] = gload<u32x4, NT_LOADS>(uniform_ptr(k_head + (pg ? at1 : at0)) + static_cast<uint32_t>(8 * j) * ts, k_off);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        t.v[e] = gload<VReg, NT_LOADS>(uniform_ptr(v_head + (e < 4 ? at0 : at1)) + static_cast<uint32_t>(e & 3) * ts, v_lane_off);
+        t.v[e] = gload<VReg, NT_LOADS>(uniform_ptr(v_head + (e < 4 ? at0 : at1)) + static_cast<uint32_t>(e & 3) * ts, v_off);
     }
   };
 
@@ -289,18 +317,20 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
   };
 
   f32x4 acc[NT][NBLK];
-  float ref[NT], sum[NT];                    // a row's reference (the same in its four lanes) and this lane's share of its sum
+  // A row's weights are relative to its base (the same in its four lanes), which moves where a logit passes it by more than the limit; before the
+  // row's first key the limit is -inf.  sum: this lane's share of the row's.
+  float base[NT], limit[NT], sum[NT];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     row_lim[nt] += sees;
-    ref[nt] = -INFINITY;
-    sum[nt] = 0.f;
+    base[nt] = sum[nt] = 0.f;
+    limit[nt] = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NBLK; ++j) acc[nt][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  // (COLLECT: pages of this chunk are parked as [page][row], all rows of the block)
+  int parked = 0;                            // COLLECT: the first tile whose log-sum-exps are still here
   auto compute = [&](int k, Tile& t) {
-    const int tok0 = (tile_first + k * NW) * kTile;
+    const int tok0 = (tile_first + k * NWH) * kTile;
     scale_lds[lane] = lane < 32 ? t.scale * p.scale_log2e : t.scale;
     wave_lds_fence();
     exchange_k(t);
@@ -316,8 +346,8 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         bf16x8 qop;
-        if constexpr (QREG) qop = __builtin_bit_cast(bf16x8, qreg[s]);
-        else qop = *reinterpret_cast<const bf16x8*>(qlds + (16 * nt + l16) * row_pitch(D) + (64 * (s >> 1) + 16 * kg + 8 * (s & 1)) * 2);
+        if constexpr (QREG) qop = __builtin_bit_cast(bf16x8, qreg[nt][s]);
+        else qop = *reinterpret_cast<const bf16x8*>(my_q + (16 * nt + l16) * row_pitch(D) + (64 * (s >> 1) + 16 * kg + 8 * (s & 1)) * 2);
 #pragma unroll
         for (int pg = 0; pg < 2; ++pg) st[nt][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kop[pg], qop, st[nt][pg], 0, 0, 0);
       }
@@ -333,42 +363,51 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
     bf16x8 pb[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float x[8];
+      float x[8];                                      // logits over the row's base (log2 units), then weights
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = st[nt][i >> 2][i & 3] * ks[i >> 2][i & 3];
+      for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(st[nt][i >> 2][i & 3], ks[i >> 2][i & 3], -base[nt]);
       if (tail) {
+        const int seen = row_lim[nt] - tok0 - 4 * kg;  // the last of this lane's tokens that the row sees
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (tok0 + 16 * (i >> 2) + 4 * kg + (i & 3) > row_lim[nt]) x[i] = -INFINITY;
+          if (16 * (i >> 2) + (i & 3) > seen) x[i] = -INFINITY;
       }
-      const float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-      if (__builtin_amdgcn_ballot_w64(top > ref[nt] + kQuantSlack) != 0) {
-        const float now = fmaxf(ref[nt], quad_rows_max(top));
-        const float alpha = now == -INFINITY ? 1.f : fast_exp2(ref[nt] - now);
-        ref[nt] = now;
+      const float top = fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(fmaxf(x[0], x[1]), x[2]), x[3]), x[4]), x[5]), x[6]), x[7]);
+      if (__builtin_amdgcn_ballot_w64(top > limit[nt]) != 0) {
+        const float over = quad_rows_max(top);         // (the four lanes of a row agree on all of this)
+        const bool first = limit[nt] == -INFINITY, none = over == -INFINITY;
+        const float up = none ? 0.f : first ? over : fmaxf(over, 0.f);
+        const float alpha = first ? 1.f : fast_exp2(-up);
+        base[nt] += up;
+        limit[nt] = none ? limit[nt] : kQuantSlack;
         sum[nt] *= alpha;
 #pragma unroll
         for (int j = 0; j < NBLK; ++j) acc[nt][j] *= alpha;
-      }
-      const float use = ref[nt] == -INFINITY ? 0.f : ref[nt];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = fast_exp2(x[i] - use);
+        for (int i = 0; i < 8; ++i) x[i] -= up;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = fast_exp2(x[i]);
       const float s0 = (x[0] + x[1]) + (x[2] + x[3]), s1 = (x[4] + x[5]) + (x[6] + x[7]);
       sum[nt] += s0 + s1;
-      if constexpr (COLLECT == 1) {
-        // log2-sum-exp2 of the tile's two pages: lanes kg = 0 have page 0's, kg = 1 page 1's
-        const float page0 = quad_rows_sum(s0), page1 = quad_rows_sum(s1);
-        const float lse = use + fast_log2(kg == 0 ? page0 : page1);
-        const int page = (tok0 - c0) / kPage + kg;
-        if (kg < 2 && 16 * nt + l16 < Rl) lse_lds[page * Rl + 16 * nt + l16] = lse;
+      if (COLLECT == 1 && p.page_lse != nullptr) {
+        // log2-sum-exp2 of the tile's two pages: the lower half wave adds up page 0's, the upper one page 1's
+        const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(s0), __float_as_uint(s1), false, false);
+        const uint32_t half0 = halves[0], half1 = halves[1];
+        const float two = __uint_as_float(half0) + __uint_as_float(half1);
+        const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(two), __float_as_uint(two), false, false);
+        const uint32_t quarter0 = rows[0], quarter1 = rows[1];
+        const float lse = base[nt] + fast_log2(__uint_as_float(quarter0) + __uint_as_float(quarter1));
+        if ((kg & 1) == 0 && 16 * nt + l16 < Rl) lse_lds[(2 * (k - parked) + (kg >> 1)) * Rl + 16 * nt + l16] = lse;
       }
       // The weights (below 2^6) times the values' scales are rounded to bf16, the second contraction's operand type: half a step of 2^-8 of
       // each weight, with random signs, beside the one of the bf16 output.  The sum has them unrounded.
+      if (tail) {                                      // (a masked token's scale may be anything)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float w = x[i] * vs[i >> 2][i & 3];
-        if (tail && x[i] == 0.f) w = 0.f;              // (a masked token's scale may be anything)
-        pb[nt][i] = static_cast<__bf16>(w);
+        for (int i = 0; i < 8; ++i) pb[nt][i] = static_cast<__bf16>(x[i] == 0.f ? 0.f : x[i] * vs[i >> 2][i & 3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pb[nt][i] = static_cast<__bf16>(x[i] * vs[i >> 2][i & 3]);
       }
       if constexpr (TIGHT) __builtin_amdgcn_sched_barrier(0);
     }
@@ -407,18 +446,47 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
 #endif
   };
 
+  // Writes the held-back log-sum-exps of the tiles before `end`: two pages a tile, the rows of a page contiguous.  (The stores are waited for:
+  // as long as one may be under way the compiler waits for everything where it wants the oldest load.)
+  auto write_parked = [&](int end) {
+    wave_lds_fence();
+    const int nblk = (n + kPage - 1) / kPage;
+    const int first = p.g, last = (p.G - 1) * p.g;     // Eq. 3: rows of the first and of the last token
+    float* const head = p.page_lse + (static_cast<int64_t>(b) * p.Hkv + h) * p.lse_pages * p.Rc;
+    for (const int from = parked; parked < end; ++parked) {
+      const int page0 = 2 * (tile_first + parked * NWH);
+      float* const dst = head + static_cast<int64_t>(page0) * p.Rc;
+      const int live = page0 + 1 < nblk ? 2 * Rl : Rl;
+      for (int e = lane; e < live; e += 64) {
+        const float lse = lse_lds[2 * (parked - from) * Rl + e];
+        if (p.Rc == Rl) {
+          dst[e] = lse;
+        } else {
+          const int page = e >= Rl ? 1 : 0, r = row0 + e - page * Rl;
+          const int ci = p.Rc == p.R ? r : r < first ? r : r >= last ? r - last + first : -1;
+          if (ci >= 0) dst[page * p.Rc + ci] = lse;
+        }
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
+    wave_lds_fence();
+  };
+
   if (ntiles > 0) issue(0, ta);
   VEGAS_TL(kTlLoadsIssued);
   if constexpr (!QREG) {                     // (every wave: the barrier)
 #pragma unroll
     for (int i = 0; i < QI; ++i) {
       const int idx = tid + i * NW * 64;
-      if (idx < 16 * NT * (D / 8)) *reinterpret_cast<u32x4*>(qlds + (idx / (D / 8)) * row_pitch(D) + (idx % (D / 8)) * 16) = qraw[i];
+#pragma unroll
+      for (int s = 0; s < kHeads; ++s)
+        if (s < HP && idx < 16 * NT * (D / 8)) *reinterpret_cast<u32x4*>(qlds + (s * 16 * NT + idx / (D / 8)) * row_pitch(D) + (idx % (D / 8)) * 16) = qraw[s][i];
     }
     __syncthreads();
   }
   VEGAS_TL(kTlQueries);
-  // ---- stream the chunk's tiles (prefetches are unconditional: the waits for a tile then count its successor's loads exactly)
+  // ---- stream the chunk's tiles, a tile ahead (the last one peeled: prefetches are unconditional, so that the waits for a tile count its
+  // successor's loads exactly.  Two or more tiles ahead change nothing, or lose what the registers cost.)
   if (ntiles > 0) {
     int k = 0;
     for (; k + 2 < ntiles; k += 2) {
@@ -426,6 +494,9 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
       compute(k, ta);
       issue(k + 2, ta);
       compute(k + 1, tb);
+      if constexpr (COLLECT == 1) {
+        if (k + 2 - parked >= qa.park_tiles && p.page_lse != nullptr) write_parked(k + 2);
+      }
     }
     if (k + 1 < ntiles) {
       issue(k + 1, tb);
@@ -433,6 +504,8 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
       ta = tb;
     }
     compute(k, ta);
+    if constexpr (COLLECT == 1)
+      if (p.page_lse != nullptr) write_parked(ntiles);
   }
   VEGAS_TL(kTlStreamed);
 
@@ -441,26 +514,11 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
   for (int nt = 0; nt < NT; ++nt) {
     const float l = quad_rows_sum(sum[nt]);
     if (kg == 0) {
-      sm_m[wave * 16 * NT + 16 * nt + l16] = ref[nt];
+      sm_m[wave * 16 * NT + 16 * nt + l16] = limit[nt] == -INFINITY ? -INFINITY : base[nt];
       sm_l[wave * 16 * NT + 16 * nt + l16] = l;
     }
   }
   __syncthreads();
-  if constexpr (COLLECT == 1) {              // the chunk's page log-sum-exps, collected rows of the block only, rows contiguous
-    const int pages = (c1 - c0 + kPage - 1) / kPage;
-    float* const dst = p.page_lse + ((static_cast<int64_t>(b) * p.Hkv + h) * p.lse_pages + c0 / kPage) * p.Rc;
-    if (p.Rc == p.R && row_blocks == 1) {
-      for (int e = tid; e < pages * Rl; e += NW * 64) dst[e] = lse_lds[e];
-    } else {
-      for (int e = tid; e < pages * Rl; e += NW * 64) {
-        const int page = e / Rl, r = row0 + e - page * Rl;
-        const int first = p.g, last = (p.G - 1) * p.g;           // Eq. 3: rows of the first and of the last token
-        const int ci = p.Rc == p.R ? r : r < first ? r : r >= last ? r - last + first : -1;
-        if (ci >= 0) dst[static_cast<int64_t>(page) * p.Rc + ci] = lse_lds[e];
-      }
-    }
-    __syncthreads();
-  }
   VEGAS_TL(kTlMerged);
 
   // ---- merge the waves, 16 rows at a time: every wave parks its rows, all threads scale and add the copies
@@ -480,16 +538,16 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
       }
     }
     __syncthreads();
-    for (int e = tid; e < rows * V4; e += NW * 64) {
-      const int row = e / V4, at = 16 * nt + row;
+    for (int e = tid; e < (HP == 1 ? rows : 16 * HP) * V4; e += NW * 64) {
+      const int s = e / (16 * V4), row = e / V4 & 15, at = 16 * nt + row;                    // (the head's waves: s, s + HP, ..)
+      if (row >= rows) continue;
       float m = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) m = fmaxf(m, sm_m[w * 16 * NT + at]);
+      for (int w = s; w < NW; w += HP) m = fmaxf(m, sm_m[w * 16 * NT + at]);
       const float use = m == -INFINITY ? 0.f : m;
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
       float l = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
+#pragma unroll 2
+      for (int w = s; w < NW; w += HP) {
         const float scale = fast_exp2(sm_m[w * 16 * NT + at] - use);
         o += *reinterpret_cast<const f32x4*>(red + (w * 16 + row) * kRed + 4 * (e % V4)) * scale;
         l += sm_l[w * 16 * NT + at] * scale;
@@ -501,10 +559,11 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
         u32x2 packed;
         packed[0] = static_cast<uint32_t>(float_to_bf16_bits(o[0] * inv)) | (static_cast<uint32_t>(float_to_bf16_bits(o[1] * inv)) << 16);
         packed[1] = static_cast<uint32_t>(float_to_bf16_bits(o[2] * inv)) | (static_cast<uint32_t>(float_to_bf16_bits(o[3] * inv)) << 16);
-        *reinterpret_cast<u32x2*>(p.out_direct + ((static_cast<int64_t>(b) * p.G + t) * p.Hq + h * p.g + (r - t * p.g)) * D + 4 * (e % V4)) = packed;
+        *reinterpret_cast<u32x2*>(p.out_direct + ((static_cast<int64_t>(b) * p.G + t) * p.Hq + (h0 + s) * p.g + (r - t * p.g)) * D + 4 * (e % V4)) = packed;
       } else {
-        *reinterpret_cast<f32x4*>(p.part_o + (pbase * p.R + r) * D + 4 * (e % V4)) = o;
-        if (e % V4 == 0) p.part_ml[pbase * p.R + r] = make_float2(m, l);
+        const int64_t at_row = (pbase + s * slots) * p.R + r;
+        *reinterpret_cast<f32x4*>(p.part_o + at_row * D + 4 * (e % V4)) = o;
+        if (e % V4 == 0) p.part_ml[at_row] = make_float2(m, l);
       }
     }
   }

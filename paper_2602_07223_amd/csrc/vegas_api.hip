@@ -607,20 +607,18 @@ int static_scratch_address(void** out) {
   return VEGAS_OK;
 }
 
-// Waves of a workgroup over an 8-bit cache: verification fills a compute unit with one, draft calls put several side by side.
-constexpr int kQuantVerifyWaves = 8, kQuantDraftWaves = 4;
-
 // For vegas_init: every kernel of attn_quant.hpp.
 template <typename F>
 void for_each_quant_kernel(F one) {
   auto rows = [&](auto dim, auto format, auto nt) {
     constexpr int D = decltype(dim)::value, FMT = decltype(format)::value, NT = decltype(nt)::value;
-    if constexpr (NT <= kQuantDraftNT) {
+    if constexpr (NT <= kQuantNT) {
       one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, true, 0, false>);
+      one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, true, 0, true>);
       one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, false, 0, false>);
+      one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 0, true>);
     }
     one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 1, true>);
-    one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 0, true>);
   };
   auto formats = [&](auto dim, auto format) {
     rows(dim, format, std::integral_constant<int, 1>{});
@@ -686,10 +684,16 @@ int for_each_lds_kernel(F f) {
 // ---- calls over an 8-bit cache (attn_quant.hpp, quant_cache.hpp)
 
 constexpr size_t kQuantLds = 150 * 1024;      // what a verification workgroup takes at most
+constexpr int kQuantParkTiles = 32;
+constexpr int64_t kQuantLargeShare = 2048;    // tokens per compute unit from which a call is bound by memory
+constexpr int kQuantShortTokens = 1536;        // sequences of a draft call that are short all the same
 
 struct QuantPlan : SplitPlan {
   int NT = 1;                        // 16-row tiles of a workgroup
+  int hp_shift = 0;                  // log2 of its KV heads
   size_t park = 0;                   // LDS in front of the queries
+  int park_tiles = 0;                // tiles whose page log-sum-exps a wave holds back
+  bool wide = false;                 // eight waves that read past the caches, planned where the batch allows
   size_t lds = 0;
 };
 
@@ -701,47 +705,59 @@ int plan_quant(const vegas_desc* d, int rows, bool collect, bool draft, QuantPla
   pl->R = rows;
   // Row blocks: as many 16-row tiles as registers hold share a tile's loads and conversions, more rows are sibling workgroups.
   const int tiles = (rows + 15) / 16;
-  const int most_tiles = draft ? kQuantDraftNT : kQuantVerifyNT;
+  const int most_tiles = draft ? kQuantNT : kQuantCollectNT;
   pl->NB = (tiles + most_tiles - 1) / most_tiles;
   pl->NT = (tiles + pl->NB - 1) / pl->NB;
-  pl->NW = draft ? kQuantDraftWaves : kQuantVerifyWaves;
-  const int unit = kTile * pl->NW;
+  // Verification, and draft calls of many tokens, have one workgroup of eight waves per compute unit that reads past the caches, and a plan
+  // by the lengths where the batch allows one; short draft calls several of four waves.  us a draft call, narrow / wide, 8 KV heads,
+  // 256 compute units, int8, 16-token pages: 12 sequences of 2080 tokens (780 per compute unit) 16.9 / 20.0, 16 of 2080 21.6 / 22.6,
+  // 4 of 16384 33.6 / 32.8, one of 65536 34.4 / 31.3, 48 of 2080 56.1 / 48.0, 16 of 4096..16384 94.8 / 66.5, 12 of 1000..48000
+  // 172 / 111; page lists of 1-token pages: 16 of 2080 19.9 / 24.8, 16 of 8192 74 / 69, 16 of 1000..8000 59 / 43.  Many short
+  // sequences want many small workgroups: 64 of 1100 32.6 / 38.3, 64 of 100..1100 20.9 / 31.6, 300 of 2000 263 / 223.
+  const int64_t share = static_cast<int64_t>(max_len) * heads / num_cu;      // tokens per compute unit, at most
+  const bool large = share >= kQuantLargeShare && (!draft || max_len > kQuantShortTokens);
+  pl->wide = !draft || large;
+  pl->NW = pl->wide ? kQuantVerifyWaves : kQuantDraftWaves;
+  pl->balanced = pl->wide && d->kv_chunk_tokens == 0 && d->batch >= 2 && d->batch <= 64 && max_len < (1 << 24);
+  // Neighbouring heads in a workgroup: whole pages are read from fewer places at a time, for as many times more partial results.  us, one head
+  // a workgroup / two / four: verification, 20 rows, one sequence of 32768 tokens 29.8 / 31.5 / 36.4, of 131072 73.0 / 68.3 / 72.3, 4 of
+  // 32768 73.9 / 70.0 / 71.3, 8 of 8192..32768 96.0 / 88.5 / 86.0, 40 of 1000..3000 62.8 / 59.0 / 55.1; draft calls, 16 of
+  // 4096..16384 75.8 / 71.3 / 66.5, 96 (unplanned) of 500..6000 145 / 141 / 172.
+  const int want = !pl->wide || !large ? 1 : pl->balanced && d->batch >= 8 ? 4 : 2;
+  pl->hp_shift = 0;
+  while ((1 << pl->hp_shift) < want && d->num_kv_heads % (2 << pl->hp_shift) == 0) ++pl->hp_shift;
+  const int HP = 1 << pl->hp_shift;
+  const int unit = kTile * (pl->NW >> pl->hp_shift);
   const int block_rows = rows < 16 * pl->NT ? rows : 16 * pl->NT;
-  const size_t tail = quant_tail_bytes(pl->NW, pl->NT, d->head_dim);
-  const int64_t per_head = static_cast<int64_t>(d->num_kv_heads) * pl->NB;
+  const size_t tail = quant_tail_bytes(pl->NW, pl->NT, d->head_dim, HP);
+  const int64_t per_head = static_cast<int64_t>(d->num_kv_heads / HP) * pl->NB;      // workgroups per slot
+  if (per_head > num_cu) pl->balanced = false;
   const int whole = (max_len + unit - 1) / unit * unit;
-  int cap = 1 << 24;                 // tokens whose page log-sum-exps a workgroup can park
-  if (collect) {
-    cap = static_cast<int>((kQuantLds - tail) / (block_rows * sizeof(float))) * kPage / unit * unit;
-    if (cap > (1 << 24)) cap = 1 << 24;
-  }
-  pl->balanced = !draft && d->kv_chunk_tokens == 0 && d->batch >= 2 && d->batch <= 64 && max_len < (1 << 24) && per_head <= num_cu;
   int chunk = d->kv_chunk_tokens;
   if (chunk == 0) {
-    const int64_t columns = heads * pl->NB;
-    int64_t splits = static_cast<int64_t>(num_cu) * (draft ? 2 : 1) / columns;
+    const int64_t columns = heads / HP * pl->NB;
+    int64_t splits = static_cast<int64_t>(num_cu) * (pl->wide ? 1 : 2) / columns;
+    if (columns >= num_cu) splits = (max_len + 2047) / 2048;     // (ragged batches that no plan evens out)
     if (splits < 1) splits = 1;
     int64_t c = (max_len + splits - 1) / splits;
+    if (!pl->wide && max_len > 4096 && c < 2 * unit) c = 2 * unit;         // (a merge of 64 partials costs more: one of 8192 tokens 11.4 -> 10.4 us)
     c = (c + unit - 1) / unit * unit;
-    const int64_t most = columns >= num_cu ? 2048 : 1 << 24;
-    if (c > most) c = most;
-    if (c > cap) c = cap;
     chunk = static_cast<int>(c);
-  } else if (chunk > cap) {
-    return VEGAS_ERR_UNSUPPORTED;
   }
-  const bool finish = draft && d->kv_chunk_tokens == 0 && max_len <= lone_workgroup_tokens(heads * pl->NB, num_cu, d->head_dim);
+  const bool finish = !pl->wide && d->kv_chunk_tokens == 0 && max_len <= lone_workgroup_tokens(heads * pl->NB, num_cu, d->head_dim);
   size_t slots = static_cast<size_t>(heads) * ((max_len + chunk - 1) / chunk);
   if (finish) chunk = whole;
   pl->chunk = chunk;
   pl->nsplit = (max_len + chunk - 1) / chunk;
   if (pl->balanced) {
-    pl->bp = batch_plan(num_cu, per_head, d->batch, max_len, unit, cap / unit, false, false, collect, d->head_dim);
-    pl->chunk = collect ? cap : unit;
+    pl->bp = batch_plan(num_cu, per_head, d->batch, max_len, unit, (1 << 24) / unit, false, false, collect, d->head_dim);
+    pl->chunk = unit;
     slots = static_cast<size_t>(d->num_kv_heads) * pl->bp.JS;
   }
   pl->lse_pages = collect ? (max_len + kPage - 1) / kPage : 0;
-  pl->park = quant_park_bytes(pl->NW, block_rows, pl->chunk, collect, d->head_dim);
+  pl->park_tiles = kQuantParkTiles;
+  while (pl->park_tiles > 2 && quant_park_bytes(pl->NW, block_rows, pl->park_tiles, collect, d->head_dim) + tail > kQuantLds) pl->park_tiles -= 2;
+  pl->park = quant_park_bytes(pl->NW, block_rows, pl->park_tiles, collect, d->head_dim);
   pl->lds = pl->park + tail;
   if (pl->balanced && pl->bp.alone && pl->lds < kLoneLds) pl->lds = kLoneLds;
   if (pl->lds > 160 * 1024) return VEGAS_ERR_UNSUPPORTED;
@@ -776,26 +792,29 @@ int page_shift_of(int page_size) {
 
 // The grid that quant_stream_kernel reads its indices off: (chunk in a group of 8, KV head and row block, group and sequence).
 int quant_groups(const QuantPlan& pl) { return pl.balanced ? 1 : (pl.nsplit + 7) / 8; }
+int quant_across(const QuantPlan& pl) { return std::min(pl.balanced ? static_cast<int>(pl.bp.JS) : pl.nsplit, 8); }
+int quant_row_blocks(const QuantPlan& pl) { return pl.NB | pl.hp_shift << 4 | quant_across(pl) << 8 | quant_groups(pl) << 12; }
 dim3 quant_grid(const QuantPlan& pl, int kv_heads, int batch) {
   const unsigned slots = pl.balanced ? pl.bp.JS : pl.nsplit;
-  return dim3(slots < 8 ? slots : 8, static_cast<unsigned>(kv_heads) * pl.NB,
+  return dim3(quant_across(pl), static_cast<unsigned>(kv_heads >> pl.hp_shift) * pl.NB,
               pl.balanced ? (slots + 7) / 8 : static_cast<unsigned>(quant_groups(pl)) * batch);
 }
-// Does a dimension of it pass what a launch takes?
+// Does a dimension of it pass what a launch takes, or the chunks the interface's bound (vegas.h, kv_chunk_tokens)?
 bool exceeds_quant_grid(const vegas_desc* d, const QuantPlan& pl) {
-  return static_cast<int64_t>(d->num_kv_heads) * pl.NB > 65535 || static_cast<int64_t>(quant_groups(pl)) * d->batch > 65535 || pl.bp.JS > 8 * 65535;
+  return exceeds_grid(pl) || static_cast<int64_t>(d->num_kv_heads) * pl.NB > 65535 || static_cast<int64_t>(quant_groups(pl)) * d->batch > 65535 || pl.bp.JS > 8 * 65535;
 }
 
 template <int D, int FMT, int NT>
 int launch_quant_nt(const vegas_desc* d, const QuantPlan& pl, const SplitParams& sp, const QuantArgs& qa, bool draft, bool collect, hipStream_t st) {
   const dim3 grid = quant_grid(pl, sp.Hkv, d->batch);
   const dim3 block(pl.NW * 64);
-  if constexpr (NT <= kQuantDraftNT) {
+  if constexpr (NT <= kQuantNT) {
+    if (draft && d->page_size != kPage && pl.wide) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, true, 0, true>, grid, block, pl.lds, st, sp, qa);
     if (draft && d->page_size != kPage) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, true, 0, false>, grid, block, pl.lds, st, sp, qa);
-    if (draft) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, false, 0, false>, grid, block, pl.lds, st, sp, qa);
+    if (!pl.wide) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, false, 0, false>, grid, block, pl.lds, st, sp, qa);
+    if (!collect) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 0, true>, grid, block, pl.lds, st, sp, qa);
   }
-  if (collect) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 1, true>, grid, block, pl.lds, st, sp, qa);
-  return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 0, true>, grid, block, pl.lds, st, sp, qa);
+  return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 1, true>, grid, block, pl.lds, st, sp, qa);
 }
 template <int D, int FMT>
 int launch_quant_rows(const vegas_desc* d, const QuantPlan& pl, const SplitParams& sp, const QuantArgs& qa, bool draft, bool collect, hipStream_t st) {
@@ -810,6 +829,7 @@ int launch_quant(const vegas_desc* d, const vegas_quant* c, const QuantPlan& pl,
   qa.scales = c->scales;
   qa.page_shift = page_shift_of(d->page_size);
   qa.park_bytes = static_cast<int32_t>(pl.park);
+  qa.park_tiles = pl.park_tiles;
   if (d->head_dim == 128)
     return c->format == VEGAS_QUANT_E4M3 ? launch_quant_rows<128, kE4m3>(d, pl, sp, qa, draft, collect, st)
                                          : launch_quant_rows<128, kInt8>(d, pl, sp, qa, draft, collect, st);
@@ -1274,7 +1294,8 @@ int vegas_verify_attention_quant(const vegas_desc* desc, const vegas_quant* cach
   SplitParams sp;
   fill_split_params(desc, pl, desc->num_queries, q, cache->k, cache->v, block_table, desc->max_blocks, seq_lens,
                     static_cast<unsigned char*>(workspace), &sp);
-  sp.row_blocks = pl.NB | quant_groups(pl) << 8;
+  sp.row_blocks = quant_row_blocks(pl);
+  if (!collect) sp.page_lse = nullptr;
   if (pl.balanced) sp.share_group = 8;                             // (eight consecutive chunks start on as many XCDs)
   rc = launch_quant(desc, cache, pl, sp, false, collect, st);
   if (rc != VEGAS_OK) return rc;
@@ -1299,9 +1320,10 @@ int vegas_draft_attention_quant(const vegas_desc* desc, const vegas_quant* cache
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   SplitParams sp;
   fill_split_params(desc, pl, 1, q, cache->k, cache->v, sel_table, desc->max_sel_blocks, sel_seq_lens, static_cast<unsigned char*>(workspace), &sp);
-  sp.row_blocks = pl.NB | quant_groups(pl) << 8;
-  const bool direct = pl.nsplit == 1;
+  sp.row_blocks = quant_row_blocks(pl);
+  const bool direct = pl.nsplit == 1 && !pl.balanced;
   if (direct) sp.out_direct = static_cast<uint16_t*>(out);
+  if (pl.balanced) sp.share_group = 8;
   rc = launch_quant(desc, cache, pl, sp, true, false, st);
   if (rc != VEGAS_OK || direct) return rc;
   return launch_combine(desc, pl, sp, out, st);

@@ -279,3 +279,45 @@ def test_lengths_and_page_ids_out_of_range_are_clamped():
     c.draft()
     c.verify(collect=1)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("lens,hq,hkv,dim,G,collect,chunk", [
+    ([12300, 40], 10, 2, 128, 4, 1, 12320), ([9000], 6, 1, 64, 4, 2, 9024), ([20000, 19000, 33], 6, 2, 128, 15, 1, 0), ([17001], 10, 2, 64, 5, 2, 17024)])
+def test_long_chunks(fmt, lens, hq, hkv, dim, G, collect, chunk):
+    """Chunks of more tiles per wave than it has page ids and log-sum-exps at hand."""
+    c = Case(lens, hq, hkv, dim, fmt, G=G, seed=21)
+    out, scores = c.verify(collect=collect, kv_chunk_tokens=chunk)
+    c.check(out, scores, collect)
+    d = Case(lens, hq, hkv, dim, fmt, seed=22)
+    d.check(d.draft(kv_chunk_tokens=chunk))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dim", [128, 64])
+@pytest.mark.parametrize("lens,hq,hkv,page", [
+    ([1000, 0, 37, 513], 8, 8, 16), ([3000, 1, 64, 0, 700, 128, 33, 2001, 90], 16, 8, 16), ([100, 2222, 5, 0, 257, 1000, 31, 64], 6, 6, 16),
+    ([800, 4000], 10, 1, 16), ([1800, 500], 34, 2, 16), ([2500], 16, 4, 16), ([17 * i % 301 for i in range(70)], 8, 4, 16),
+    ([3000, 1, 64, 0, 700, 128, 33, 2001, 90], 16, 8, 1), ([100, 2222, 5, 0, 257, 1000, 31, 64], 6, 2, 4), ([2500], 16, 4, 8),
+    ([17 * i % 301 for i in range(70)], 4, 2, 2), ([900, 333], 100, 1, 1)])
+def test_bounds_of_large_draft_calls(fmt, dim, lens, hq, hkv, page):
+    """The lengths may lie far below the call's bound, which is what its workgroups and its plan are chosen by."""
+    units = torch.cuda.get_device_properties(0).multi_processor_count
+    bound = max(2048 * units // (len(lens) * hkv) + 77, max(lens) + 1, 1600)
+    c = Case(lens, hq, hkv, dim, fmt, page=page, seed=31, spare_width=bound // page + 1, max_len=bound)
+    c.check(c.draft())
+    c.check(c.draft(kv_chunk_tokens=256))
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dim", [128, 64])
+@pytest.mark.parametrize("lens,hq,hkv,G", [
+    ([1000, 0, 37, 513], 8, 8, 5), ([3000, 1, 64, 0, 700, 128, 33, 2001, 90], 64, 8, 5), ([100, 2222, 5, 0, 257, 1000, 31, 64], 18, 6, 6),
+    ([800, 4000], 10, 1, 4), ([2500], 16, 4, 11), ([17 * i % 301 for i in range(70)], 8, 4, 3)])
+def test_bounds_of_large_verification_calls(fmt, dim, lens, hq, hkv, G):
+    units = torch.cuda.get_device_properties(0).multi_processor_count
+    bound = max(2048 * units // (len(lens) * hkv) + 77, max(lens) + 1)
+    c = Case(lens, hq, hkv, dim, fmt, G=G, seed=32, spare_width=bound // 16 + 1, max_len=bound)
+    for collect in (0, 1, 2):
+        out, scores = c.verify(collect=collect)
+        c.check(out, scores, collect)

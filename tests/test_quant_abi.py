@@ -101,7 +101,6 @@ def test_verification_refusals():
     refused(lambda: verify(d=desc(score_metric=2)), vb.VEGAS_ERR_SHAPE)
     refused(lambda: verify(d=desc(collect_rows=0, window=128)), vb.VEGAS_ERR_UNSUPPORTED)
     refused(lambda: verify(d=desc(score_metric=vb.METRIC_TOKEN_LOGITS)), vb.VEGAS_ERR_UNSUPPORTED)
-    refused(lambda: verify(d=desc(num_queries=32, kv_chunk_tokens=32768)), vb.VEGAS_ERR_UNSUPPORTED)   # more scores than a workgroup parks
     refused(lambda: verify(d=desc(kv_chunk_tokens=100)), vb.VEGAS_ERR_SHAPE)
     refused(lambda: verify(wb=1024), vb.VEGAS_ERR_WORKSPACE)
     refused(lambda: verify(ws=None), vb.VEGAS_ERR_WORKSPACE)
