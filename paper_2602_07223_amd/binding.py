@@ -188,8 +188,8 @@ def load_library(path: Optional[str] = None):
 # handle (harness): an iteration of 4096 tokens 42.6 / 33.8 (GPU 38), of 32768 56 / 43, a verification of one launch 6.8 / 4.5 (7.3 ->
 # 6.4 a call).
 def _ptr(x) -> Optional[int]:
-    if x is None:
-        return None
+    if type(x) is int or x is None:
+        return x
     if isinstance(x, int):
         return x
     return int(x.data_ptr())
@@ -218,9 +218,11 @@ def _fits(where: str, name: str, x, nbytes: int) -> Optional[int]:
     passed, refuse any that is smaller than what the descriptor lets the kernels touch.  Returns the address."""
     if x is None or isinstance(x, int):
         return x
-    have = _avail_bytes(x)                          # (the storage's: it may have been resized under a tensor that still has its shape)
-    if have < nbytes:
-        raise ValueError(f"{where}: {name} spans {have} bytes, the descriptor needs {nbytes}")
+    # (the storage's bytes: it may have been resized under a tensor that still has its shape)
+    if x.untyped_storage().nbytes() < nbytes or x.storage_offset():
+        have = _avail_bytes(x)
+        if have < nbytes:
+            raise ValueError(f"{where}: {name} spans {have} bytes, the descriptor needs {nbytes}")
     return x.data_ptr()
 
 
@@ -520,24 +522,47 @@ def quant_extent_bytes(desc: VegasDesc) -> int:
 
 def quant_scales_bytes(desc: VegasDesc) -> int:
     """Bytes of the scales of a cache with desc.num_pages pages of desc.page_size tokens."""
-    pages16 = -(-int(desc.num_pages) * desc.page_size // 16)
-    return pages16 * desc.num_kv_heads * 32 * 4
+    return ((desc.num_pages * desc.page_size + 15) // 16) * desc.num_kv_heads * 128
 
 
+def _spans(*tensors):
+    """Bytes that each spans (None: nothing there, or a raw address, which the caller answers for)."""
+    return tuple(None if x is None or isinstance(x, int) else _avail_bytes(x) for x in tensors)
+
+
+# The handles below hold the addresses that their tensors had when they were made, and what those spanned then: a call compares
+# integers instead of asking the tensors again (0.4 us each; a decoding step's append has eight of them).
 def make_quant(k, v, scales, fmt: int) -> VegasQuant:
     """Handle of an 8-bit cache: code tensors, scales and format (QUANT_*).  Keeps the tensors alive."""
     c = VegasQuant(_ptr(k), _ptr(v), _ptr(scales), fmt, 0)
     c.tensors = (k, v, scales)
+    c.spans, c.fits = _spans(k, v, scales), None
     return c
 
 
 def _quant_fits(where: str, desc: VegasDesc, cache: VegasQuant) -> None:
-    k, v, scales = cache.tensors
-    if isinstance(k, int):
+    """(Once per descriptor's content: its fields are a microsecond to read.)"""
+    content = bytes(desc)
+    if cache.fits == content:
         return
-    _fits(where, "k", k, quant_extent_bytes(desc))
-    _fits(where, "v", v, quant_extent_bytes(desc))
-    _fits(where, "scales", scales, quant_scales_bytes(desc))
+    need, scales = quant_extent_bytes(desc), quant_scales_bytes(desc)
+    for name, have, n in zip(("k", "v", "scales"), cache.spans, (need, need, scales)):
+        if have is not None and have < n:
+            raise ValueError(f"{where}: {name} spans {have} bytes, the descriptor needs {n}")
+    cache.fits = content
+
+
+def _new_tokens_fit(where: str, desc: VegasDesc, tokens: VegasNewTokens) -> None:
+    content = bytes(desc) + bytes(tokens)
+    if tokens.fits == content:
+        return
+    rows, kv_row, q_row = desc.batch * tokens.num_new, desc.num_kv_heads * desc.head_dim, desc.num_q_heads * desc.head_dim
+    kv = _rows_bytes(rows, tokens.kv_token_stride or kv_row, kv_row)
+    needs = (kv, kv, _rows_bytes(rows, tokens.q_token_stride or q_row, q_row), _rows_bytes(rows, tokens.q_out_token_stride or q_row, q_row), 4 * desc.batch)
+    for name, have, n in zip(("k", "v", "q", "q_out", "new_lens"), tokens.spans, needs):
+        if have is not None and have < n:
+            raise ValueError(f"{where}: {name} spans {have} bytes, the descriptor needs {n}")
+    tokens.fits = content
 
 
 def vegas_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROPE_SCALE_NONE, factor: float = 1.0,
@@ -573,14 +598,13 @@ def vegas_rotate(rope: VegasRope, head_dim: int, num_tokens: int, num_heads: int
     for raw addresses)."""
     xs, os_ = x_strides, out_strides
     if xs is None:
-        xs = (num_heads * head_dim, head_dim) if isinstance(x, int) else (x.stride(-3), x.stride(-2))
+        xs = (num_heads * head_dim, head_dim) if isinstance(x, int) else x.stride()[-3:-1]
     if os_ is None:
-        os_ = (num_heads * head_dim, head_dim) if isinstance(out, int) else (out.stride(-3), out.stride(-2))
+        os_ = (num_heads * head_dim, head_dim) if isinstance(out, int) else out.stride()[-3:-1]
     x_at, out_at, positions_at = x, out, positions
     if not (isinstance(x, int) and isinstance(out, int)):
-        width = (num_heads - 1) * xs[1] + head_dim
-        x_at = _fits("vegas_rotate", "x", x, _rows_bytes(num_tokens, xs[0], width))
-        out_at = _fits("vegas_rotate", "out", out, _rows_bytes(num_tokens, os_[0], (num_heads - 1) * os_[1] + head_dim))
+        x_at = _fits("vegas_rotate", "x", x, _rows_bytes(num_tokens, xs[0], (num_heads - 1) * xs[1] + head_dim))
+        out_at = x_at if out is x else _fits("vegas_rotate", "out", out, _rows_bytes(num_tokens, os_[0], (num_heads - 1) * os_[1] + head_dim))
         positions_at = _fits("vegas_rotate", "positions", positions, num_tokens * 4)
     rc = (_lib or load_library()).vegas_rotate(_byref(rope) if rope is not None else None, int(head_dim), int(num_tokens), int(num_heads), _ptr(positions_at), _ptr(x_at),
                                                xs[0], xs[1], _ptr(out_at), os_[0], os_[1], _stream(stream))
@@ -593,6 +617,7 @@ def make_new_tokens(k, v, num_new: int, *, q=None, q_out=None, new_lens=None, kv
     """New rows of a batch for vegas_append_quant (0: contiguous rows).  Keeps the tensors alive."""
     n = VegasNewTokens(_ptr(k), _ptr(v), _ptr(q), _ptr(q_out), _ptr(new_lens), kv_token_stride, q_token_stride, q_out_token_stride, num_new, 0)
     n.tensors = (k, v, q, q_out, new_lens)
+    n.spans, n.fits = _spans(k, v, q, q_out, new_lens), None
     return n
 
 
@@ -602,17 +627,14 @@ def vegas_append_quant(desc: VegasDesc, cache: VegasQuant, rope: Optional[VegasR
     if not (isinstance(block_table, int) and isinstance(seq_lens, int)):
         d, where = desc, "vegas_append_quant"
         _quant_fits(where, d, cache)
-        k, v, q, q_out, new_lens = tokens.tensors
-        rows, kv_row, q_row = d.batch * tokens.num_new, d.num_kv_heads * d.head_dim, d.num_q_heads * d.head_dim
-        for name, x, stride, width in (("k", k, tokens.kv_token_stride, kv_row), ("v", v, tokens.kv_token_stride, kv_row),
-                                       ("q", q, tokens.q_token_stride, q_row), ("q_out", q_out, tokens.q_out_token_stride, q_row)):
-            _fits(where, name, x, _rows_bytes(rows, stride or width, width))
-        _fits(where, "new_lens", new_lens, d.batch * 4)
-        block_table_at = _fits(where, "block_table", block_table, d.batch * d.max_blocks * 4)
-        seq_lens_at = _fits(where, "seq_lens", seq_lens, d.batch * 4)
-        seq_lens_out_at = _fits(where, "seq_lens_out", seq_lens_out, d.batch * 4)
-        sel_table_at = _fits(where, "sel_table", sel_table, d.batch * d.max_sel_blocks * 4)
-        sel_seq_lens_at = _fits(where, "sel_seq_lens", sel_seq_lens, d.batch * 4)
+        _new_tokens_fit(where, d, tokens)
+        batch = d.batch
+        block_table_at = _fits(where, "block_table", block_table, batch * d.max_blocks * 4)
+        seq_lens_at = _fits(where, "seq_lens", seq_lens, batch * 4)
+        seq_lens_out_at = seq_lens_at if seq_lens_out is seq_lens else _fits(where, "seq_lens_out", seq_lens_out, batch * 4)
+        if sel_table is not None:
+            sel_table_at = _fits(where, "sel_table", sel_table, batch * d.max_sel_blocks * 4)
+            sel_seq_lens_at = _fits(where, "sel_seq_lens", sel_seq_lens, batch * 4)
     rc = (_lib or load_library()).vegas_append_quant(
         _byref(desc), _byref(cache), _byref(rope) if rope is not None else None, _byref(tokens), _ptr(block_table_at), _ptr(seq_lens_at),
         _ptr(seq_lens_out_at), _ptr(sel_table_at), _ptr(sel_seq_lens_at), int(sel_page_size), _stream(stream))
