@@ -296,7 +296,7 @@ def _handles(s):
     if kind == "read":
         s["k_out"], s["v_out"] = (torch.zeros((B, T, Hkv, D), **bf16) for _ in range(2))
         return
-    s["workspace"] = torch.empty(vb.vegas_workspace_bytes(s["desc"]), dtype=torch.uint8, device=dev)
+    s["workspace"] = torch.empty(vb.vegas_quant_workspace_bytes(s["desc"]), dtype=torch.uint8, device=dev)
     s["out"] = torch.empty(s["q"].shape, **bf16)
     s["scores"] = torch.empty((B, width), dtype=torch.float32, device=dev) if c["collect"] else None
 
