@@ -389,7 +389,7 @@ typedef struct vegas_new_tokens {
   const void* q;               /* bf16 [B, num_new, H_q, D], or NULL: rotated into q_out in the same launch (needs `rope`) */
   void* q_out;                 /* NULL exactly if q is; may be q itself (same stride) */
   const int32_t* new_lens;     /* DEVICE int32 [B]: how many of its num_new rows sequence b has (clamped to 0 .. num_new; rows
-                                  past them are padding: not read, q_out not written), or NULL: all */
+                                  past them are padding: of no effect, q_out not written), or NULL: all */
   int64_t kv_token_stride;     /* elements between the tokens of k and of v (a multiple of 8; 0: H_kv * D); a sequence's rows follow */
   int64_t q_token_stride;      /* the last sequence's.  Likewise for q and q_out (0: H_q * D) */
   int64_t q_out_token_stride;

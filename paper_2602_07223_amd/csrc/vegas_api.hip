@@ -1410,6 +1410,8 @@ int vegas_append_quant(const vegas_desc* desc, const vegas_quant* cache, const v
   const int64_t kv_token = tokens->kv_token_stride ? tokens->kv_token_stride : kv_row;
   const int64_t q_token = tokens->q_token_stride ? tokens->q_token_stride : q_row;
   const int64_t q_out_token = tokens->q_out_token_stride ? tokens->q_out_token_stride : q_row;
+  const intptr_t ahead = reinterpret_cast<intptr_t>(seq_lens_out) - reinterpret_cast<intptr_t>(seq_lens);
+  if (ahead != 0 && std::abs(ahead) < static_cast<intptr_t>(desc->batch) * 4) return VEGAS_ERR_SHAPE;   // (neither in place nor apart)
   if (kv_token < kv_row || q_token < q_row || q_out_token < q_row) return VEGAS_ERR_SHAPE;
   if (tokens->q && tokens->q == tokens->q_out && q_token != q_out_token) return VEGAS_ERR_SHAPE;
   if (!aligned16(tokens->k) || !aligned16(tokens->v) || !aligned16(tokens->q) || !aligned16(tokens->q_out) || ((kv_token | q_token | q_out_token) % 8))
@@ -1451,13 +1453,16 @@ int vegas_append_quant(const vegas_desc* desc, const vegas_quant* cache, const v
   const bool in_place = seq_lens == seq_lens_out;
   const bool one_workgroup = in_place && static_cast<int64_t>(p.T) * all <= kOneWorkgroupSteps;
   p.seq_lens_out = in_place && !one_workgroup ? nullptr : seq_lens_out;
-  p.steps = wave_steps(static_cast<int64_t>(desc->batch) * p.T, all);
-  p.tokens = p.T >= 64 ? kPage : 4;          // (a page's scales are written by one workgroup, or two)
-  const dim3 grid = one_workgroup ? dim3(1, 1, desc->batch) : dim3((p.T + p.tokens - 1) / p.tokens, (all + p.steps - 1) / p.steps, desc->batch);
+  const bool many = !one_workgroup && p.T >= 4 * kAppendTokens;
+  const int wg_tokens = many ? kAppendTokens : 4;           // of a workgroup of four waves
+  p.steps = wave_steps(static_cast<int64_t>(desc->batch) * p.T * 4 / wg_tokens, all);
+  if (many && p.steps > kAppendSteps) p.steps = kAppendSteps;
+  const dim3 grid = one_workgroup ? dim3(1, 1, desc->batch) : dim3((p.T + wg_tokens - 1) / wg_tokens, (all + p.steps - 1) / p.steps, desc->batch);
   hipStream_t st = static_cast<hipStream_t>(hip_stream);
   auto launch = [&](auto dim, auto format) {
     constexpr int D = decltype(dim)::value, FMT = decltype(format)::value;
     if (one_workgroup) hipLaunchKernelGGL((append_quant_kernel<D, FMT, true>), grid, dim3(1024), 0, st, p);
+    else if (many) hipLaunchKernelGGL((append_pages_kernel<D, FMT>), grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL((append_quant_kernel<D, FMT, false>), grid, dim3(256), 0, st, p);
   };
   auto by_format = [&](auto dim) {

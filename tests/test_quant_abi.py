@@ -147,6 +147,7 @@ def test_append_refusals():
     refused(lambda: append(r=rope(), n=tokens(q=A, q_out=A, q_token_stride=8192)), vb.VEGAS_ERR_SHAPE)   # in place with two strides
     refused(lambda: append(n=tokens(k=A + 8)), vb.VEGAS_ERR_ALIGN)
     refused(lambda: append(d=desc(page_size=8)), vb.VEGAS_ERR_UNSUPPORTED)
+    refused(lambda: append(lens=A, after=A + 4), vb.VEGAS_ERR_SHAPE)                            # neither in place nor apart
     refused(lambda: append(sel=A), vb.VEGAS_ERR_NULL)
     refused(lambda: append(sel_lens=A), vb.VEGAS_ERR_NULL)
     refused(lambda: append(sel=A, sel_lens=A, page=4), vb.VEGAS_ERR_UNSUPPORTED)
