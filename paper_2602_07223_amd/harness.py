@@ -13,6 +13,7 @@ from . import binding as vb
 from .synth import LayerInputs
 
 PAGE = 16
+CACHE_FORMATS = {"e4m3": (vb.QUANT_E4M3, torch.float8_e4m3fn), "int8": (vb.QUANT_INT8, torch.int8)}    # 8-bit caches
 
 
 def bf16_to_device(bits: np.ndarray, device) -> torch.Tensor:
@@ -38,6 +39,7 @@ class DeviceLayer:
     k_new: Optional[torch.Tensor] = None     # bf16 [steps, B, 1, Hkv, D]: rows the live drafting phase appends
     v_new: Optional[torch.Tensor] = None
     seq_lens_live: Optional[torch.Tensor] = None   # int32 [B]: the lengths the live drafting phase advances
+    quant: Optional[vb.VegasQuant] = None          # the same cache in 8 bits (k_cache and v_cache then hold its codes)
 
     @staticmethod
     def upload(L: LayerInputs, device="cuda:0") -> "DeviceLayer":
@@ -50,6 +52,27 @@ class DeviceLayer:
             dl.seq_lens_live = dl.seq_lens.clone()
         return dl
 
+    def quantised(self, fmt: str) -> "DeviceLayer":
+        """The layer over an 8-bit cache ("e4m3" or "int8"): a copy whose pool holds this one's rows quantised, page by page (each page
+        is appended as a sequence of 16 tokens, so pages that no table names are quantised as well)."""
+        code, dtype = CACHE_FORMATS[fmt]
+        pages, _, heads, dim = self.k_cache.shape
+        dev = self.k_cache.device
+        k, v = (torch.empty(self.k_cache.shape, dtype=dtype, device=dev) for _ in range(2))
+        scales = torch.empty((pages, heads, 2, PAGE), dtype=torch.float32, device=dev)
+        quant = vb.make_quant(k, v, scales, code)
+        most = 32768                         # sequences of a call (a dimension of its grid)
+        for first in range(0, pages, most):
+            n = min(most, pages - first)
+            desc = vb.make_desc(batch=n, num_q_heads=heads, num_kv_heads=heads, num_queries=0, max_blocks=1, max_sel_blocks=0, max_seq_len=PAGE,
+                                num_pages=pages, softmax_scale=1.0, head_dim=dim)
+            table = torch.arange(first, first + n, dtype=torch.int32, device=dev)
+            lens = torch.zeros(n, dtype=torch.int32, device=dev)
+            tokens = vb.make_new_tokens(self.k_cache[first:first + n], self.v_cache[first:first + n], PAGE)
+            vb.vegas_append_quant(desc, quant, None, tokens, table, lens, torch.empty_like(lens), stream=torch.cuda.current_stream(dev).cuda_stream)
+        lens = self.seq_lens_live.clone() if self.seq_lens_live is not None else None
+        return dataclasses.replace(self, k_cache=k, v_cache=v, quant=quant, seq_lens_live=lens)
+
 
 class VegasPath:
     """One layer's verify -> select -> draft calls with preallocated outputs and workspace."""
@@ -59,10 +82,16 @@ class VegasPath:
                  collect_rows: int = vb.COLLECT_ALL_ROWS, head_dim: int = 128, device="cuda:0",
                  verify_chunk: int = 0, draft_chunk: int = 0, max_sel_blocks: int = 0,
                  score_metric: int = vb.METRIC_PAGE_WEIGHTS, token_granular: bool = False, window: int = 0,
-                 growth: int = 0):
+                 growth: int = 0, cache_format: str = "bf16"):
         """token_granular: the paper's own variant -- verification collects averaged logits per token,
         selection picks single tokens, drafting walks one-token pages (Sec. 3.3, Sec. 4).
-        window > 0: verification of a banded layer (local masking; needs collect_rows = COLLECT_NONE)."""
+        window > 0: verification of a banded layer (local masking; needs collect_rows = COLLECT_NONE).
+        cache_format "e4m3" or "int8": the calls run over an 8-bit cache (DeviceLayer.quantised); pages only, without local masking."""
+        if cache_format != "bf16" and cache_format not in CACHE_FORMATS:
+            raise ValueError(f"unknown cache format {cache_format!r}")
+        self.quantised = cache_format != "bf16"
+        if self.quantised and (token_granular or window or score_metric != vb.METRIC_PAGE_WEIGHTS):
+            raise ValueError("an 8-bit cache is verified with page weights and without local masking")
         self.device = torch.device(device)
         self.token_granular = token_granular
         if token_granular:
@@ -90,9 +119,10 @@ class VegasPath:
             draft_len = min(self.max_sel_blocks * PAGE, max_blocks * PAGE)
             self.desc_draft = vb.make_desc(max_seq_len=draft_len, collect_rows=vb.COLLECT_NONE,
                                            kv_chunk_tokens=draft_chunk, **common)
-        nbytes = max(vb.vegas_workspace_bytes(self.desc_verify), vb.vegas_workspace_bytes(self.desc_draft))
+        workspace_bytes = vb.vegas_quant_workspace_bytes if self.quantised else vb.vegas_workspace_bytes
+        nbytes = max(workspace_bytes(self.desc_verify), workspace_bytes(self.desc_draft))
         if nbytes == 0:
-            raise ValueError("descriptor rejected by vegas_workspace_bytes")
+            raise ValueError(f"descriptor rejected by {workspace_bytes.__name__}")
         dev = self.device
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=dev)
         self.out_verify = torch.empty((batch, num_queries, num_q_heads, head_dim), dtype=torch.bfloat16, device=dev)
@@ -128,9 +158,14 @@ class VegasPath:
     # call stays at a few microseconds: at batch 1 the kernels are that short.
     def _addrs(self, dl: DeviceLayer):
         a = dl.__dict__.get("_addrs")
+        if (dl.quant is not None) != self.quantised:
+            raise ValueError("the layer's cache is not of the path's format")
         if a is None:
             # checked once per layer, since the calls below hand over addresses: both descriptors' cache extents
             for desc in (self.desc_verify, self.desc_draft):
+                if dl.quant is not None:
+                    vb._quant_fits("VegasPath", desc, dl.quant)
+                    continue
                 need = vb.cache_extent_bytes(desc)
                 for name in ("k_cache", "v_cache"):
                     have = vb._avail_bytes(getattr(dl, name))
@@ -159,6 +194,12 @@ class VegasPath:
 
     def verify(self, dl: DeviceLayer, stream=None, stages: int = 0) -> None:
         a, o = self._addrs(dl), self._own()
+        if self.quantised:
+            if stages:
+                raise ValueError("calls over an 8-bit cache have no stages")
+            vb.vegas_verify_attention_quant(self.desc_verify, dl.quant, a["qv"], a["bt"], a["sl"], o["ov"], o["bs"], o["ws"],
+                                            self.stream() if stream is None else stream, o["wsn"])
+            return
         vb.vegas_verify_attention(self.desc_verify, a["qv"], a["k"], a["v"], a["bt"], a["sl"], o["ov"], o["bs"], o["ws"],
                                   self.stream() if stream is None else stream, o["wsn"], stages)
 
@@ -175,6 +216,12 @@ class VegasPath:
 
     def draft(self, dl: DeviceLayer, step: int, stream=None, stages: int = 0) -> None:
         a, o = self._addrs(dl), self._own()
+        if self.quantised:
+            if stages:
+                raise ValueError("calls over an 8-bit cache have no stages")
+            vb.vegas_draft_attention_quant(self.desc_draft, dl.quant, a["qd"][step], o["st"], o["ssl"], o["od"][step], o["ws"],
+                                           self.stream() if stream is None else stream, o["wsn"])
+            return
         vb.vegas_draft_attention(self.desc_draft, a["qd"][step], a["k"], a["v"], o["st"], o["ssl"], o["od"][step], o["ws"],
                                  self.stream() if stream is None else stream, o["wsn"], stages)
 
@@ -183,7 +230,8 @@ class VegasPath:
         then per draft step the new token's K/V is appended, the selection grows by it (Sec. 3.2, last sentence)
         and the draft call attends over the grown selection.  The live lengths are rewound first (one small device
         copy), so every iteration starts from the same state; the appended slots are simply overwritten.
-        fused: append, growth and draft as one call (vegas_draft_step) instead of three."""
+        fused: append, growth and draft as one call (vegas_draft_step) instead of three.  Over an 8-bit cache there are two: an append
+        that grows the selection, and the draft call."""
         st = self.stream()
         a, o = self._addrs(dl), self._own()
         dl.seq_lens_live.copy_(dl.seq_lens)
@@ -192,6 +240,14 @@ class VegasPath:
         sll = dl.seq_lens_live.data_ptr()
         row = dl.k_new[0].numel() * dl.k_new.element_size()
         k_new, v_new = dl.k_new.data_ptr(), dl.v_new.data_ptr()
+        if self.quantised:
+            steps = dl.__dict__.get("_steps")
+            if steps is None:
+                steps = dl._steps = [vb.make_new_tokens(dl.k_new[s], dl.v_new[s], 1) for s in range(self.G)]
+            for s in range(self.G):
+                vb.vegas_append_quant(self.desc_append, dl.quant, None, steps[s], a["bt"], sll, sll, o["st"], o["ssl"], PAGE, stream=st)
+                self.draft(dl, s, st)
+            return
         for s in range(self.G):
             if fused:
                 vb.vegas_draft_step(self.desc_append, self.desc_draft, a["qd"][s], k_new + s * row, v_new + s * row, a["bt"], sll,
