@@ -19,10 +19,12 @@
 //     usual rescaling of the outputs, and the reduction over the four lanes of a row, is seldom met.
 // What bounds it: memory from 64 MB on, latencies below.  A 32-token tile of a head is 8.25 KB (D = 128), half of the bf16 cache's, and costs 80
 // conversions (e4m3; int8 192) and per 16 rows 16 MFMAs and about 90 vector instructions; a copy that only loads its tiles takes 270 us
-// where the kernel with 40 rows takes 285.  Loads run a whole tile ahead in a second set of registers; three to five tiles ahead
+// where the kernel with 40 rows took 285.  Loads run a whole tile ahead in a second set of registers; three to five tiles ahead
 // were no faster.  Captured calls with their merges: verification of 16 sequences of 8192..65536 tokens, 40 rows, 8 KV heads (1.26 GB)
-// 284 us, without scores 226 (5.5 TB/s; the log-sum-exps, 47 MB written and read again, make the difference), 20 rows and 36864 tokens
-// each 218 (5.7 TB/s); one sequence of 32768, 20 rows 26.4; draft calls, 12 of 1000..48000 (642 MB) 111 (5.8 TB/s), one of 2080 6.9.
+// 266 us, without scores 229 (5.5 TB/s; the log-sum-exps, 47 MB written and read again, make the difference), 20 rows 245; one sequence of
+// 32768, 20 rows 25.8 (first request to first tile 6 us, the stream at 6.8 TB/s, 2.5 to merge the waves, then the scores' launch);
+// draft calls, 12 of 1000..48000 (642 MB, int8) 115 (5.6 TB/s), 16 of 8192 over single tokens 71 (3.9 TB/s: the scales of
+// a token and head are two sectors of their line), one of 2080 6.6.
 // TOKENS: the page list has pages of fewer than 16 tokens (page_shift): every lane works out the address of one token
 // of the tile, the wave shares them through LDS.
 #pragma once
@@ -103,6 +105,7 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
   static_assert(D == 128 || D == 64, "head dimension");
   static_assert(!TOKENS || COLLECT == 0, "page lists are not scored");
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ int progress[NW];               // tiles that a wave has begun
   constexpr int KL = D / 64;                 // K loads of a page
   constexpr int KS = D / 32;                 // steps of the first contraction
   constexpr int NBLK = D / 16;               // 16-row blocks of the output, codes of a V load
@@ -487,9 +490,20 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
   VEGAS_TL(kTlQueries);
   // ---- stream the chunk's tiles, a tile ahead (the last one peeled: prefetches are unconditional, so that the waits for a tile count its
   // successor's loads exactly.  Two or more tiles ahead change nothing, or lose what the registers cost.)
+  // Of two waves on a SIMD the older one's requests go first: waves 4 .. 7 of eight were a tenth behind at the end.  Whoever is ahead gives way
+  // (16 sequences of 8192..65536 tokens, 40 rows 282 -> 266 us, without scores 237 -> 228; 12 of 1000..48000 drafted 119.5 -> 115.3).
+  if constexpr (WIDE) {
+    if (lane == 0) progress[wave] = 0;
+  }
   if (ntiles > 0) {
     int k = 0;
     for (; k + 2 < ntiles; k += 2) {
+      if constexpr (WIDE) {
+        volatile int* const at = progress;
+        at[wave] = k;
+        if (k > __builtin_amdgcn_readfirstlane(at[wave ^ (NW / 2)])) __builtin_amdgcn_s_setprio(0);
+        else __builtin_amdgcn_s_setprio(1);
+      }
       issue(k + 1, tb);
       compute(k, ta);
       issue(k + 2, ta);
@@ -523,34 +537,24 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
 
   // ---- merge the waves, 16 rows at a time: every wave parks its rows, all threads scale and add the copies
   constexpr int V4 = D / 4;
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int rows = min(16, Rl - 16 * nt);
-    if (rows <= 0) break;
-    if (nt > 0) __syncthreads();
-    if (l16 < rows) {
-      float* dst = red + (wave * 16 + l16) * kRed;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int d0 = NBLK * (4 * kg + i);
-        *reinterpret_cast<f32x4*>(dst + d0) = f32x4{acc[nt][0][i], acc[nt][1][i], acc[nt][2][i], acc[nt][3][i]};
-        if constexpr (NBLK == 8) *reinterpret_cast<f32x4*>(dst + d0 + 4) = f32x4{acc[nt][4 % NBLK][i], acc[nt][5 % NBLK][i], acc[nt][6 % NBLK][i], acc[nt][7 % NBLK][i]};
-      }
-    }
-    __syncthreads();
+  auto add_waves = [&](auto waves, int nt, int rows) {
+    constexpr int N = decltype(waves)::value;
     for (int e = tid; e < (HP == 1 ? rows : 16 * HP) * V4; e += NW * 64) {
       const int s = e / (16 * V4), row = e / V4 & 15, at = 16 * nt + row;                    // (the head's waves: s, s + HP, ..)
       if (row >= rows) continue;
-      float m = -INFINITY;
-      for (int w = s; w < NW; w += HP) m = fmaxf(m, sm_m[w * 16 * NT + at]);
+      float scale[N], m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int j = 0; j < N; ++j) scale[j] = sm_m[(s + (j << hp_shift)) * 16 * NT + at];
+#pragma unroll
+      for (int j = 0; j < N; ++j) m = fmaxf(m, scale[j]);
       const float use = m == -INFINITY ? 0.f : m;
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
-      float l = 0.f;
-#pragma unroll 2
-      for (int w = s; w < NW; w += HP) {
-        const float scale = fast_exp2(sm_m[w * 16 * NT + at] - use);
-        o += *reinterpret_cast<const f32x4*>(red + (w * 16 + row) * kRed + 4 * (e % V4)) * scale;
-        l += sm_l[w * 16 * NT + at] * scale;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int w = s + (j << hp_shift);
+        scale[j] = fast_exp2(scale[j] - use);
+        o += *reinterpret_cast<const f32x4*>(red + (w * 16 + row) * kRed + 4 * (e % V4)) * scale[j];
+        l += sm_l[w * 16 * NT + at] * scale[j];
       }
       const int r = row0 + at;
       if (p.out_direct != nullptr) {         // the only chunk: the bf16 rows (Eq. 1); a row with no visible key: zeros
@@ -566,6 +570,30 @@ __global__ __launch_bounds__(NW * 64, 2) void quant_stream_kernel(VEGAS_SPLIT_HO
         if (e % V4 == 0) p.part_ml[at_row] = make_float2(m, l);
       }
     }
+  };
+  auto add_copies = [&](int nt, int rows) {
+    if constexpr (WIDE) {
+      if (hp_shift == 2) return add_waves(std::integral_constant<int, NW / 4>{}, nt, rows);
+      if (hp_shift == 1) return add_waves(std::integral_constant<int, NW / 2>{}, nt, rows);
+    }
+    add_waves(std::integral_constant<int, NW>{}, nt, rows);
+  };
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int rows = min(16, Rl - 16 * nt);
+    if (rows <= 0) break;
+    if (nt > 0) __syncthreads();
+    if (l16 < rows) {
+      float* dst = red + (wave * 16 + l16) * kRed;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int d0 = NBLK * (4 * kg + i);
+        *reinterpret_cast<f32x4*>(dst + d0) = f32x4{acc[nt][0][i], acc[nt][1][i], acc[nt][2][i], acc[nt][3][i]};
+        if constexpr (NBLK == 8) *reinterpret_cast<f32x4*>(dst + d0 + 4) = f32x4{acc[nt][4 % NBLK][i], acc[nt][5 % NBLK][i], acc[nt][6 % NBLK][i], acc[nt][7 % NBLK][i]};
+      }
+    }
+    __syncthreads();
+    add_copies(nt, rows);
   }
   VEGAS_TL(kTlExit);
   VEGAS_TL_FLUSH(p.timeline, NW);
