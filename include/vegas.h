@@ -438,7 +438,8 @@ int vegas_verify_attention_quant(const vegas_desc* desc, const vegas_quant* cach
 /*
  * vegas_draft_attention over an 8-bit cache: attention of one new token per sequence over a page list of 1, 2, 4, 8 or 16 tokens
  * per page, split over the list's length and joined.  With a block table for a list (max_sel_blocks its row stride, max_seq_len the
- * longest sequence) it is a decoding step of full attention.  `workspace`: at least vegas_quant_workspace_bytes(desc) bytes.
+ * longest sequence) it is a decoding step of full attention.  Calls of many tokens on a batch of 2..64 sequences get their chunks from
+ * the lengths, as verification does (kv_chunk_tokens).  `workspace`: at least vegas_quant_workspace_bytes(desc) bytes.
  */
 int vegas_draft_attention_quant(const vegas_desc* desc, const vegas_quant* cache, const void* q, const int32_t* sel_table,
                                 const int32_t* sel_seq_lens, void* out, void* workspace, size_t workspace_bytes,

@@ -540,16 +540,20 @@ def make_quant(k, v, scales, fmt: int) -> VegasQuant:
     return c
 
 
-def _quant_fits(where: str, desc: VegasDesc, cache: VegasQuant) -> None:
-    """(Once per descriptor's content: its fields are a microsecond to read.)"""
+def _quant_fits(where: str, desc: VegasDesc, cache: VegasQuant):
+    """Refuses a cache smaller than the descriptor's; returns bytes of (lengths, block table or block scores, page list, one row of queries per
+    sequence, num_queries rows).  (Once per descriptor's content: its fields are a microsecond to read.)"""
     content = bytes(desc)
     if cache.fits == content:
-        return
+        return cache.sizes
     need, scales = quant_extent_bytes(desc), quant_scales_bytes(desc)
     for name, have, n in zip(("k", "v", "scales"), cache.spans, (need, need, scales)):
         if have is not None and have < n:
             raise ValueError(f"{where}: {name} spans {have} bytes, the descriptor needs {n}")
+    row = desc.batch * desc.num_q_heads * desc.head_dim * 2
+    cache.sizes = (4 * desc.batch, 4 * desc.batch * desc.max_blocks, 4 * desc.batch * desc.max_sel_blocks, row, row * desc.num_queries)
     cache.fits = content
+    return cache.sizes
 
 
 def _new_tokens_fit(where: str, desc: VegasDesc, tokens: VegasNewTokens) -> None:
@@ -625,16 +629,15 @@ def vegas_append_quant(desc: VegasDesc, cache: VegasQuant, rope: Optional[VegasR
                        seq_lens_out, sel_table=None, sel_seq_lens=None, sel_page_size: int = 16, stream=None) -> None:
     block_table_at, seq_lens_at, seq_lens_out_at, sel_table_at, sel_seq_lens_at = block_table, seq_lens, seq_lens_out, sel_table, sel_seq_lens
     if not (isinstance(block_table, int) and isinstance(seq_lens, int)):
-        d, where = desc, "vegas_append_quant"
-        _quant_fits(where, d, cache)
-        _new_tokens_fit(where, d, tokens)
-        batch = d.batch
-        block_table_at = _fits(where, "block_table", block_table, batch * d.max_blocks * 4)
-        seq_lens_at = _fits(where, "seq_lens", seq_lens, batch * 4)
-        seq_lens_out_at = seq_lens_at if seq_lens_out is seq_lens else _fits(where, "seq_lens_out", seq_lens_out, batch * 4)
+        where = "vegas_append_quant"
+        lens_bytes, table_bytes, list_bytes = _quant_fits(where, desc, cache)[:3]
+        _new_tokens_fit(where, desc, tokens)
+        block_table_at = _fits(where, "block_table", block_table, table_bytes)
+        seq_lens_at = _fits(where, "seq_lens", seq_lens, lens_bytes)
+        seq_lens_out_at = seq_lens_at if seq_lens_out is seq_lens else _fits(where, "seq_lens_out", seq_lens_out, lens_bytes)
         if sel_table is not None:
-            sel_table_at = _fits(where, "sel_table", sel_table, batch * d.max_sel_blocks * 4)
-            sel_seq_lens_at = _fits(where, "sel_seq_lens", sel_seq_lens, batch * 4)
+            sel_table_at = _fits(where, "sel_table", sel_table, list_bytes)
+            sel_seq_lens_at = _fits(where, "sel_seq_lens", sel_seq_lens, lens_bytes)
     rc = (_lib or load_library()).vegas_append_quant(
         _byref(desc), _byref(cache), _byref(rope) if rope is not None else None, _byref(tokens), _ptr(block_table_at), _ptr(seq_lens_at),
         _ptr(seq_lens_out_at), _ptr(sel_table_at), _ptr(sel_seq_lens_at), int(sel_page_size), _stream(stream))
@@ -645,12 +648,12 @@ def vegas_append_quant(desc: VegasDesc, cache: VegasQuant, rope: Optional[VegasR
 def vegas_read_quant(desc: VegasDesc, cache: VegasQuant, table, lens, first, num_tokens: int, k_out, v_out, stream=None) -> None:
     table_at, lens_at, first_at, k_out_at, v_out_at = table, lens, first, k_out, v_out
     if not (isinstance(table, int) and isinstance(k_out, int)):
-        d, where = desc, "vegas_read_quant"
-        _quant_fits(where, d, cache)
-        rows = d.batch * int(num_tokens) * d.num_kv_heads * d.head_dim * 2
-        table_at = _fits(where, "table", table, d.batch * d.max_sel_blocks * 4)
-        lens_at = _fits(where, "lens", lens, d.batch * 4)
-        first_at = _fits(where, "first", first, d.batch * 4)
+        where = "vegas_read_quant"
+        lens_bytes, _, list_bytes = _quant_fits(where, desc, cache)[:3]
+        rows = desc.batch * int(num_tokens) * desc.num_kv_heads * desc.head_dim * 2
+        table_at = _fits(where, "table", table, list_bytes)
+        lens_at = _fits(where, "lens", lens, lens_bytes)
+        first_at = _fits(where, "first", first, lens_bytes)
         k_out_at = _fits(where, "k_out", k_out, rows)
         v_out_at = _fits(where, "v_out", v_out, rows)
     rc = (_lib or load_library()).vegas_read_quant(_byref(desc), _byref(cache), _ptr(table_at), _ptr(lens_at), _ptr(first_at), int(num_tokens),
@@ -668,15 +671,14 @@ def vegas_verify_attention_quant(desc: VegasDesc, cache: VegasQuant, q, block_ta
     wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
     q_at, block_table_at, seq_lens_at, out_at, block_scores_at = q, block_table, seq_lens, out, block_scores
     if not (isinstance(q, int) and isinstance(block_table, int)):
-        d, where = desc, "vegas_verify_attention_quant"
-        _quant_fits(where, d, cache)
-        rows = d.batch * d.num_queries * d.num_q_heads * d.head_dim * 2
+        where = "vegas_verify_attention_quant"
+        lens_bytes, table_bytes, _, _, rows = _quant_fits(where, desc, cache)
         q_at = _fits(where, "q", q, rows)
         out_at = _fits(where, "out", out, rows)
-        block_table_at = _fits(where, "block_table", block_table, d.batch * d.max_blocks * 4)
-        seq_lens_at = _fits(where, "seq_lens", seq_lens, d.batch * 4)
-        if d.collect_rows != COLLECT_NONE:
-            block_scores_at = _fits(where, "block_scores", block_scores, d.batch * d.max_blocks * 4)
+        block_table_at = _fits(where, "block_table", block_table, table_bytes)
+        seq_lens_at = _fits(where, "seq_lens", seq_lens, lens_bytes)
+        if desc.collect_rows != COLLECT_NONE:
+            block_scores_at = _fits(where, "block_scores", block_scores, table_bytes)
     rc = (_lib or load_library()).vegas_verify_attention_quant(
         _byref(desc), _byref(cache), _ptr(q_at), _ptr(block_table_at), _ptr(seq_lens_at), _ptr(out_at), _ptr(block_scores_at), _ptr(workspace),
         wb, _stream(stream))
@@ -689,13 +691,12 @@ def vegas_draft_attention_quant(desc: VegasDesc, cache: VegasQuant, q, sel_table
     wb = workspace_bytes if workspace_bytes is not None else (_nbytes(workspace) if workspace is not None else 0)
     q_at, sel_table_at, sel_seq_lens_at, out_at = q, sel_table, sel_seq_lens, out
     if not (isinstance(q, int) and isinstance(sel_table, int)):
-        d, where = desc, "vegas_draft_attention_quant"
-        _quant_fits(where, d, cache)
-        rows = d.batch * d.num_q_heads * d.head_dim * 2
-        q_at = _fits(where, "q", q, rows)
-        out_at = _fits(where, "out", out, rows)
-        sel_table_at = _fits(where, "sel_table", sel_table, d.batch * d.max_sel_blocks * 4)
-        sel_seq_lens_at = _fits(where, "sel_seq_lens", sel_seq_lens, d.batch * 4)
+        where = "vegas_draft_attention_quant"
+        lens_bytes, _, list_bytes, row, _ = _quant_fits(where, desc, cache)
+        q_at = _fits(where, "q", q, row)
+        out_at = _fits(where, "out", out, row)
+        sel_table_at = _fits(where, "sel_table", sel_table, list_bytes)
+        sel_seq_lens_at = _fits(where, "sel_seq_lens", sel_seq_lens, lens_bytes)
     rc = (_lib or load_library()).vegas_draft_attention_quant(_byref(desc), _byref(cache), _ptr(q_at), _ptr(sel_table_at), _ptr(sel_seq_lens_at), _ptr(out_at),
                                                               _ptr(workspace), wb, _stream(stream))
     if rc != VEGAS_OK:
