@@ -43,7 +43,7 @@ struct QuantArgs {
   int32_t park_tiles;        // COLLECT: tiles whose log-sum-exps a wave holds back (even)
 };
 
-constexpr int kQuantCollectNT = 3, kQuantNT = 2;       // 16-row tiles of a workgroup that collects, and of others, at most: what registers hold
+constexpr int kQuantVerifyNT = 3, kQuantDraftNT = 2;  // 16-row tiles of a workgroup, at most: what registers hold
 constexpr int kQuantVerifyWaves = 8, kQuantDraftWaves = 4;      // waves of a workgroup (wide ones, of long calls, and narrow ones)
 constexpr int kQuantHeads = 4;                // KV heads of a workgroup, at most
 constexpr float kQuantSlack = 6.f;           // log2 of how far weights may pass 1

@@ -612,7 +612,7 @@ template <typename F>
 void for_each_quant_kernel(F one) {
   auto rows = [&](auto dim, auto format, auto nt) {
     constexpr int D = decltype(dim)::value, FMT = decltype(format)::value, NT = decltype(nt)::value;
-    if constexpr (NT <= kQuantNT) {
+    if constexpr (NT <= kQuantDraftNT) {
       one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, true, 0, false>);
       one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, true, 0, true>);
       one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, false, 0, false>);
@@ -705,7 +705,7 @@ int plan_quant(const vegas_desc* d, int rows, bool collect, bool draft, QuantPla
   pl->R = rows;
   // Row blocks: as many 16-row tiles as registers hold share a tile's loads and conversions, more rows are sibling workgroups.
   const int tiles = (rows + 15) / 16;
-  const int most_tiles = draft ? kQuantNT : kQuantCollectNT;
+  const int most_tiles = draft ? kQuantDraftNT : kQuantVerifyNT;
   pl->NB = (tiles + most_tiles - 1) / most_tiles;
   pl->NT = (tiles + pl->NB - 1) / pl->NB;
   // Verification, and draft calls of many tokens, have one workgroup of eight waves per compute unit that reads past the caches, and a plan
@@ -733,7 +733,7 @@ int plan_quant(const vegas_desc* d, int rows, bool collect, bool draft, QuantPla
   const int64_t per_head = static_cast<int64_t>(d->num_kv_heads / HP) * pl->NB;      // workgroups per slot
   if (per_head > num_cu) pl->balanced = false;
   const int whole = (max_len + unit - 1) / unit * unit;
-  int chunk = d->kv_chunk_tokens;
+  int chunk = d->kv_chunk_tokens < whole ? d->kv_chunk_tokens : whole;       // (any multiple of 32 is a caller's right: sums with it have to fit)
   if (chunk == 0) {
     const int64_t columns = heads / HP * pl->NB;
     int64_t splits = static_cast<int64_t>(num_cu) * (pl->wide ? 1 : 2) / columns;
@@ -808,12 +808,13 @@ template <int D, int FMT, int NT>
 int launch_quant_nt(const vegas_desc* d, const QuantPlan& pl, const SplitParams& sp, const QuantArgs& qa, bool draft, bool collect, hipStream_t st) {
   const dim3 grid = quant_grid(pl, sp.Hkv, d->batch);
   const dim3 block(pl.NW * 64);
-  if constexpr (NT <= kQuantNT) {
+  if constexpr (NT <= kQuantDraftNT) {
     if (draft && d->page_size != kPage && pl.wide) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, true, 0, true>, grid, block, pl.lds, st, sp, qa);
     if (draft && d->page_size != kPage) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, true, 0, false>, grid, block, pl.lds, st, sp, qa);
     if (!pl.wide) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantDraftWaves, false, 0, false>, grid, block, pl.lds, st, sp, qa);
     if (!collect) return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 0, true>, grid, block, pl.lds, st, sp, qa);
   }
+  // (Three tiles without scores: this instance too, with nowhere to put them.  One of its own needs more registers than there are.)
   return launch_one(quant_stream_kernel<D, FMT, NT, kQuantVerifyWaves, false, 1, true>, grid, block, pl.lds, st, sp, qa);
 }
 template <int D, int FMT>

@@ -287,3 +287,10 @@ def test_yarn_by_parts():
 ])
 def test_frequency_refusals(args, status):
     refused(lambda: vb.vegas_rope_frequencies(*args), status)
+
+
+@pytest.mark.parametrize("num_queries", [1, 5])
+def test_any_chunk_length_up_to_the_type_s_end(num_queries):
+    """A chunk longer than the bound on the lengths is one chunk."""
+    over = dict(num_queries=num_queries, max_blocks=64, max_sel_blocks=64, max_seq_len=1000)
+    assert vb.vegas_quant_workspace_bytes(desc(kv_chunk_tokens=2 ** 31 - 32, **over)) == vb.vegas_quant_workspace_bytes(desc(kv_chunk_tokens=1024, **over)) > 0
