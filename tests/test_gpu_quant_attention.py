@@ -321,3 +321,19 @@ def test_bounds_of_large_verification_calls(fmt, dim, lens, hq, hkv, G):
     for collect in (0, 1, 2):
         out, scores = c.verify(collect=collect)
         c.check(out, scores, collect)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("lens,hq,hkv,dim,G", [
+    ([700, 0, 37, 513, 64, 1500, 9, 128, 333], 64, 8, 128, 7), ([700, 0, 37, 513, 64, 1500, 9, 128, 333], 32, 4, 64, 16), ([1200], 64, 8, 128, 16),
+    ([900, 130], 16, 2, 128, 15), ([11 * i % 257 for i in range(66)], 28, 4, 64, 9)])
+def test_row_blocks_of_large_verification_calls(fmt, lens, hq, hkv, dim, G):
+    """More rows than a workgroup has, beside neighbouring heads in it."""
+    units = torch.cuda.get_device_properties(0).multi_processor_count
+    bound = max(2048 * units // (len(lens) * hkv) + 77, max(lens) + 1)
+    c = Case(lens, hq, hkv, dim, fmt, G=G, seed=33, spare_width=bound // 16 + 1, max_len=bound)
+    for collect in (0, 1, 2):
+        out, scores = c.verify(collect=collect)
+        c.check(out, scores, collect)
+    out, scores = c.verify(collect=1, kv_chunk_tokens=512)
+    c.check(out, scores, 1)
