@@ -241,11 +241,9 @@ class VegasPath:
         row = dl.k_new[0].numel() * dl.k_new.element_size()
         k_new, v_new = dl.k_new.data_ptr(), dl.v_new.data_ptr()
         if self.quantised:
-            steps = dl.__dict__.get("_steps")
-            if steps is None:
-                steps = dl._steps = [vb.make_new_tokens(dl.k_new[s], dl.v_new[s], 1) for s in range(self.G)]
             for s in range(self.G):
-                vb.vegas_append_quant(self.desc_append, dl.quant, None, steps[s], a["bt"], sll, sll, o["st"], o["ssl"], PAGE, stream=st)
+                new = vb.make_new_tokens(k_new + s * row, v_new + s * row, 1)
+                vb.vegas_append_quant(self.desc_append, dl.quant, None, new, a["bt"], sll, sll, o["st"], o["ssl"], PAGE, stream=st)
                 self.draft(dl, s, st)
             return
         for s in range(self.G):
